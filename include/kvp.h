@@ -413,6 +413,165 @@ KVP_API int32_t kvp_compose_noalloc(const void *pool_k, const void *pool_v, int6
                                     const int32_t *delta, void *cache_k, void *cache_v, int64_t cache_rows,
                                     void *stream, char *err, int32_t err_cap);
 
+/* ---- norms and rotation of new tokens; a cache in pages -------------------------------------------------- */
+
+/*
+ * Rotary positions as models use them: element pair i of the first rotary_dim elements of a head is rotated by
+ * position * f_i radians and multiplied by `magnitude`; the elements behind them stay as they are.
+ *   f_i = theta^(-2i/rotary_dim), or inv_freq[i]; for long contexts, with scale > 1:
+ *   original_positions = 0: f_i / scale (positions are interpolated);
+ *   original_positions = L: with t = L f_i / 2 pi the turns that pair i makes over the original context, pairs of at least
+ *   high_rotations turns keep f_i, pairs of at most low_rotations get f_i / scale, and between them
+ *   w f_i + (1 - w) f_i / scale with w = (t - low_rotations) / (high_rotations - low_rotations).  (1, 4) with magnitude 1 is
+ *   the scaling of Llama 3.1, (1, 32) with magnitude 0.1 ln(scale) + 1 that of YaRN (Peng et al. 2023, Section 3).
+ * Angles are formed in double precision, position * f_i / 2 pi reduced to a part of a turn there.
+ */
+typedef struct kvp_rope {
+    int32_t struct_bytes;       /* = sizeof(kvp_rope)                                                 */
+    int32_t pairing;            /* 0: pairs (i, i + rotary_dim/2);  1: pairs (2i, 2i + 1)             */
+    int32_t rotary_dim;         /* a multiple of 16 up to head_dim; 0: no rotation                    */
+    int32_t reserved;           /* 0                                                                  */
+    double theta;
+    const double *inv_freq;     /* optional host array [rotary_dim/2], in place of theta              */
+    double scale;               /* >= 1                                                               */
+    double original_positions, low_rotations, high_rotations;
+    double magnitude;           /* > 0                                                                */
+} kvp_rope;
+
+/* The frequencies f_i of `rope` after scaling, inv_freq: host [rotary_dim/2] (what kvp_config.inv_freq takes, so that
+   packets are re-based with the model's scaled frequencies).  Errors: INVALID. */
+KVP_API int32_t kvp_rope_frequencies(const kvp_rope *rope, double *inv_freq);
+
+/*
+ * New tokens as a layer's projections give them.  Strides are in elements, {token, head}; the elements of a head lie side
+ * by side.  A fused projection's output is taken as it is: q, k and v are then pointers into it with its token stride.
+ * Pointers are 16-byte aligned and strides multiples of 16 bytes.
+ */
+typedef struct kvp_tokens {
+    int32_t struct_bytes;       /* = sizeof(kvp_tokens)                                               */
+    int32_t n_tokens;           /* >= 0                                                               */
+    int32_t n_q_heads, n_kv_heads;
+    const void *q, *k, *v;      /* device; q or k may be NULL (its output too); v only for kvp_cache_append */
+    void *q_out, *k_out;        /* device; may be q and k themselves (with the same strides)          */
+    int64_t q_stride[2], k_stride[2], v_stride[2], q_out_stride[2], k_out_stride[2];
+    const int32_t *positions;   /* device [n_tokens]; may be NULL without rotation                    */
+    const int32_t *slots;       /* device [n_tokens], kvp_cache_append: page * page_size + row of each token;
+                                   a token whose slot lies outside the store is not written           */
+    const void *q_weight, *k_weight; /* device [head_dim], the context's dtype; NULL: no norm          */
+    double eps;                 /* of the norms                                                       */
+} kvp_tokens;
+
+/*
+ * Norm of every q and k head over its head_dim elements, x / sqrt(mean(x^2) + eps) * weight (where there is a weight), then
+ * the rotation to the token's position; fp32 throughout, rounded once.  What kvp_query_prefill takes as q and k_new for
+ * models that norm them, rotate a part of the head or scale their frequencies.
+ *   dtype, head_dim   as in kvp_config; device: CUDA ordinal that the pointers lie on (it need not be the current one)
+ *   rope              NULL: no rotation
+ * Errors (text: kvp_cache_last_error(NULL)): INVALID, CUDA.
+ */
+KVP_API int32_t kvp_norm_rope(int32_t device, int32_t dtype, int32_t head_dim, const kvp_tokens *tokens, const kvp_rope *rope,
+                      void *stream);
+
+/*
+ * A cache in pages: what a composed cache becomes when it lives longer than its assembly - answers are generated into it,
+ * forked from it, rows are thinned out.  K and V are [layer][page][kv head][row][d] or [layer][page][row][kv head][d], or
+ * anything else that four strides describe; a request is a list of pages (row j lies in its page j / page_size) and a
+ * length.  Lists and lengths are the caller's, in device memory, so that a captured step can be replayed while they grow.
+ * A page number outside the store is never followed: rows on such a page are not there.
+ *
+ * A cache is used by one host thread at a time.  kvp_cache_attend uses the cache's workspace: attend calls of one cache have
+ * to be ordered among each other (captured ones too); everything else only by the rows that it reads and writes.
+ */
+typedef struct kvp_cache kvp_cache;
+
+typedef struct kvp_cache_config {
+    int32_t struct_bytes;       /* = sizeof(kvp_cache_config)                                         */
+    int32_t device;             /* CUDA ordinal; -1 = host only: pages are counted, nothing runs      */
+    int32_t n_layers, n_q_heads, n_kv_heads;
+    int32_t head_dim;           /* 64 or 128                                                          */
+    int32_t dtype;              /* KVP_DTYPE_*                                                        */
+    int32_t page_size;          /* rows of a page, >= 1; page_size * n_kv_heads <= 2^24               */
+    int32_t n_pages;            /* n_pages * page_size < 2^31                                         */
+    int32_t max_batch;          /* requests of one kvp_cache_attend                                   */
+    int64_t layer_stride, page_stride, head_stride, row_stride;   /* elements; multiples of 16 bytes  */
+    double softmax_scale;       /* 0 -> 1/sqrt(head_dim)                                              */
+    void *k, *v;                /* device, 16-byte aligned                                            */
+    void *workspace;            /* device, 256-byte aligned                                           */
+    uint64_t workspace_bytes;   /* at least kvp_cache_workspace_bytes(cfg)                            */
+} kvp_cache_config;
+
+/* Workspace size that the configuration needs.  0 if cfg is invalid. */
+KVP_API uint64_t kvp_cache_workspace_bytes(const kvp_cache_config *cfg);
+
+/* k, v and the workspace are borrowed; the workspace's counters are zeroed here (synchronised before return).
+   Errors: INVALID, CAPACITY (workspace too small), CUDA; text: kvp_cache_last_error(NULL). */
+KVP_API int32_t kvp_cache_create(const kvp_cache_config *cfg, kvp_cache **out);
+KVP_API int32_t kvp_cache_destroy(kvp_cache *cache);
+
+/*
+ * Norms and rotation as kvp_norm_rope, and the keys and values of `layer` go to their slots in the same pass (k_out may be
+ * NULL then; q too: a composed cache from kvp_export_cache is taken over without rope and weights).  Slots of one call must
+ * differ.  Errors: INVALID, STATE (host only), CUDA.
+ */
+KVP_API int32_t kvp_cache_append(kvp_cache *cache, int32_t layer, const kvp_tokens *tokens, const kvp_rope *rope, void *stream);
+
+/*
+ * Attention of one new token per request over its rows first[b] <= j < lens[b] of `layer` (its own row among them, once
+ * appended): softmax in fp32, q head h reads kv head h / (Hq/Hkv).
+ *   q      device, {batch, head} strides in elements; out likewise.  16-byte aligned, strides multiples of 16 bytes
+ *   table  device [batch][table_cols] with row stride table_stride: page numbers
+ *   lens, first   device [batch]; first may be NULL (0).  Lengths beyond table_cols pages end there.  A request without a
+ *          row gets zeros and an lse of minus infinity
+ *   lse    device float [batch][n_q_heads] or NULL
+ * The work is shared out on the device, by the lengths that lie there when the kernel runs.
+ * Errors: INVALID, CAPACITY (batch > max_batch), STATE (host only), CUDA.
+ */
+KVP_API int32_t kvp_cache_attend(kvp_cache *cache, int32_t layer, int32_t batch, const void *q, const int64_t *q_stride,
+                         const int32_t *table, int64_t table_stride, int32_t table_cols, const int32_t *lens,
+                         const int32_t *first, void *out, const int64_t *out_stride, float *lse, void *stream);
+
+/*
+ * Rows [0, rows[i]) (rows NULL: all) of page src[i] to page dst[i], in all layers and heads, K and V.  Host arrays, read before
+ * the call returns.  Errors: INVALID (a page or row count out of range, a page written twice, or written and read), STATE
+ * (host only; a page to be written is shared), CUDA.
+ */
+KVP_API int32_t kvp_cache_copy(kvp_cache *cache, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *rows,
+                       void *stream);
+
+/*
+ * Thinning out: row i < n_kept[b] of the pages in new_table[b] becomes row kept[b][l][h][i] of those in table[b], for every
+ * layer l and kv head h, K and V.  Keys keep the rotation of the position they were cached at, so each head may keep rows of
+ * its own; later tokens go on at positions of the caller's (kvp_tokens.positions).
+ *   kept      device, strides kept_stride = {request, layer, head} in elements (0: the same list for all), max_kept entries
+ *   n_kept    device [batch], at most max_kept
+ * A kept row at or behind lens[b], or on a page outside the store, leaves its place as it is.  The pages of new_table must
+ * not be among those that are read.  Errors: INVALID, STATE (host only), CUDA.
+ */
+KVP_API int32_t kvp_cache_compact(kvp_cache *cache, int32_t batch, const int32_t *table, int64_t table_stride, int32_t table_cols,
+                          const int32_t *lens, const int32_t *new_table, int64_t new_stride, int32_t new_cols,
+                          const int32_t *kept, const int64_t *kept_stride, int32_t max_kept, const int32_t *n_kept, void *stream);
+
+/*
+ * Who holds which pages (host side; nothing runs on the device but a fork's copy).  A page that is taken has one holder, every
+ * share adds one, every release takes one away; without a holder it is free again, and may be taken while work that reads it
+ * is still enqueued: such work has to lie in front, on the same stream or otherwise.  All or nothing: after an error every
+ * page is held as before.
+ *   take     n free pages.  Errors: INVALID, CAPACITY
+ *   share, release   Errors: INVALID (page number, n), STATE (a page has no holder, or not enough for what is released)
+ *   fork     n_forks more lists for the first n_tokens rows of `pages`: whole pages are shared, the last one, if it is not
+ *            full, is copied to a new page for each (one launch).  forks: host [n_forks][pages of n_tokens rows]
+ */
+KVP_API int32_t kvp_cache_take(kvp_cache *cache, int32_t n, int32_t *pages);
+KVP_API int32_t kvp_cache_share(kvp_cache *cache, int32_t n, const int32_t *pages);
+KVP_API int32_t kvp_cache_release(kvp_cache *cache, int32_t n, const int32_t *pages);
+KVP_API int32_t kvp_cache_fork(kvp_cache *cache, int32_t n_tokens, const int32_t *pages, int32_t n_forks, int32_t *forks,
+                       void *stream);
+KVP_API int32_t kvp_cache_free_pages(kvp_cache *cache, int32_t *n);
+
+/* Text of the last error on this cache; with NULL, of this thread's last kvp_cache_create, kvp_norm_rope or
+   kvp_rope_frequencies that failed. */
+KVP_API const char *kvp_cache_last_error(kvp_cache *cache);
+
 /* Text of the last error on this context (owned by ctx; "" if none).  With ctx == NULL: the reason
    the last kvp_create on this thread failed. */
 KVP_API const char *kvp_last_error(kvp_ctx *ctx);

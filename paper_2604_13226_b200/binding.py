@@ -43,6 +43,37 @@ class kvp_config(ctypes.Structure):
     ]
 
 
+class kvp_rope(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_int32), ("pairing", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+        ("reserved", ctypes.c_int32), ("theta", ctypes.c_double), ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+        ("scale", ctypes.c_double), ("original_positions", ctypes.c_double), ("low_rotations", ctypes.c_double),
+        ("high_rotations", ctypes.c_double), ("magnitude", ctypes.c_double),
+    ]
+
+
+class kvp_tokens(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 2),
+        ("k_stride", ctypes.c_int64 * 2), ("v_stride", ctypes.c_int64 * 2), ("q_out_stride", ctypes.c_int64 * 2),
+        ("k_out_stride", ctypes.c_int64 * 2), ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_double),
+    ]
+
+
+class kvp_cache_config(ctypes.Structure):
+    _fields_ = [
+        ("struct_bytes", ctypes.c_int32), ("device", ctypes.c_int32), ("n_layers", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_batch", ctypes.c_int32),
+        ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64), ("softmax_scale", ctypes.c_double), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_uint64),
+    ]
+
+
 _lib = None
 
 
@@ -56,6 +87,7 @@ def lib() -> ctypes.CDLL:
         path = _build.build()
     L = ctypes.CDLL(path)
     vp, i32, u32, u64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64
+    i64 = ctypes.c_int64
     pi32 = ctypes.POINTER(ctypes.c_int32)
     pcfg = ctypes.POINTER(kvp_config)
     sig = {
@@ -87,6 +119,21 @@ def lib() -> ctypes.CDLL:
         "kvp_last_error": (ctypes.c_char_p, [vp]),
         "kvp_compose_noalloc": (i32, [vp, vp, ctypes.c_int64, i32, i32, i32, i32, ctypes.c_double, i32, pi32, pi32, pi32,
                                       vp, vp, ctypes.c_int64, vp, ctypes.c_char_p, i32]),
+        "kvp_rope_frequencies": (i32, [ctypes.POINTER(kvp_rope), ctypes.POINTER(ctypes.c_double)]),
+        "kvp_norm_rope": (i32, [i32, i32, i32, vp, vp, vp]),
+        "kvp_cache_workspace_bytes": (u64, [ctypes.POINTER(kvp_cache_config)]),
+        "kvp_cache_create": (i32, [ctypes.POINTER(kvp_cache_config), ctypes.POINTER(vp)]),
+        "kvp_cache_destroy": (i32, [vp]),
+        "kvp_cache_append": (i32, [vp, i32, vp, vp, vp]),
+        "kvp_cache_attend": (i32, [vp, i32, i32, vp, vp, vp, i64, i32, vp, vp, vp, vp, vp, vp]),
+        "kvp_cache_copy": (i32, [vp, i32, vp, vp, vp, vp]),
+        "kvp_cache_compact": (i32, [vp, i32, vp, i64, i32, vp, vp, i64, i32, vp, vp, i32, vp, vp]),
+        "kvp_cache_take": (i32, [vp, i32, vp]),
+        "kvp_cache_share": (i32, [vp, i32, vp]),
+        "kvp_cache_release": (i32, [vp, i32, vp]),
+        "kvp_cache_fork": (i32, [vp, i32, vp, i32, vp, vp]),
+        "kvp_cache_free_pages": (i32, [vp, pi32]),
+        "kvp_cache_last_error": (ctypes.c_char_p, [vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)          # AttributeError if the library lacks a declared symbol
@@ -100,7 +147,10 @@ EXPORTED = ["kvp_version", "kvp_token_bytes", "kvp_workspace_bytes", "kvp_create
             "kvp_register_packet", "kvp_register_packet_compressed", "kvp_register_packet_host", "kvp_evict_packet",
             "kvp_register_adapter", "kvp_assemble", "kvp_assemble_at", "kvp_partial_bytes", "kvp_merge_partials", "kvp_query_prefill", "kvp_query_prefill_ragged",
             "kvp_export_plan", "kvp_export_cache", "kvp_export_schedule", "kvp_segment_mass", "kvp_status_word", "kvp_last_launch", "kvp_tune",
-            "kvp_kernel_times", "kvp_last_error", "kvp_compose_noalloc"]
+            "kvp_kernel_times", "kvp_last_error", "kvp_compose_noalloc", "kvp_rope_frequencies", "kvp_norm_rope",
+            "kvp_cache_workspace_bytes", "kvp_cache_create", "kvp_cache_destroy", "kvp_cache_append", "kvp_cache_attend",
+            "kvp_cache_copy", "kvp_cache_compact", "kvp_cache_take", "kvp_cache_share", "kvp_cache_release", "kvp_cache_fork",
+            "kvp_cache_free_pages", "kvp_cache_last_error"]
 
 
 def _i32_array(xs: Sequence[int]):
@@ -363,3 +413,238 @@ def compose_noalloc(pool_k: int, pool_v: int, pool_rows: int, n_planes: int, hea
                                _ptr(cache_k), _ptr(cache_v), cache_rows, st, err, 256)
     if rc != KVP_OK:
         raise KvpError(rc, err.value.decode())
+
+
+# ---- norms and rotation of new tokens; a cache in pages ------------------------------------------------------
+
+class Rope:
+    """``kvp_rope``: rotary positions of the first ``rotary_dim`` elements of a head, scaled for long contexts or not."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, theta: float = 10000.0, pairing: int = 0,
+                 inv_freq: Optional[Sequence[float]] = None, scale: float = 1.0, original_positions: float = 0.0,
+                 low_rotations: float = 1.0, high_rotations: float = 4.0, magnitude: float = 1.0):
+        r = kvp_rope()
+        r.struct_bytes = ctypes.sizeof(kvp_rope)
+        r.pairing, r.rotary_dim = pairing, head_dim if rotary_dim is None else rotary_dim
+        r.theta, r.scale, r.original_positions = theta, scale, original_positions
+        r.low_rotations, r.high_rotations, r.magnitude = low_rotations, high_rotations, magnitude
+        self._inv_freq = None
+        if inv_freq is not None:
+            if len(inv_freq) != r.rotary_dim // 2:
+                raise KvpError(1, f"rope: {len(inv_freq)} frequencies for rotary_dim {r.rotary_dim}")
+            self._inv_freq = (ctypes.c_double * max(1, len(inv_freq)))(*inv_freq)
+            r.inv_freq = ctypes.cast(self._inv_freq, ctypes.POINTER(ctypes.c_double))
+        self.struct, self.address = r, ctypes.addressof(r)
+
+    def frequencies(self) -> List[float]:
+        """The frequencies after scaling, as ``Context(inv_freq=...)`` takes them."""
+        out = (ctypes.c_double * max(1, self.struct.rotary_dim // 2))()
+        _checked(lib().kvp_rope_frequencies(ctypes.byref(self.struct), out))
+        return list(out)[:self.struct.rotary_dim // 2]
+
+
+def _checked(rc: int, cache=None):
+    if rc != KVP_OK:
+        raise KvpError(rc, (lib().kvp_cache_last_error(cache) or b"").decode())
+
+
+def _raw_stream(index: int, stream) -> int:
+    import torch
+    if stream is not None:
+        return stream.cuda_stream
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(index) if get else torch.cuda.current_stream(index).cuda_stream
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise KvpError(1, f"{t.dtype} is neither float32 nor bfloat16")
+    return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
+
+
+def _rows(t, like, name: str, heads: int = 0):
+    """(address, token stride, head stride) of [token][head][d] like ``like`` = (dtype, device, head_dim)."""
+    if t.dim() != 3 or t.dtype != like[0] or t.device != like[1] or t.shape[2] != like[2] or (heads and t.shape[1] != heads):
+        raise KvpError(1, f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise KvpError(1, f"{name}: the elements of a head do not lie side by side")
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _ints(t, device, name: str, *shape):
+    import torch
+    if t.dtype != torch.int32 or t.device != device or t.dim() != len(shape) or any(s >= 0 and s != n for s, n in zip(shape, t.shape)):
+        raise KvpError(1, f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise KvpError(1, f"{name}: entries do not lie side by side")
+    return t.data_ptr()
+
+
+def _tokens(like, q, k, v, q_out, k_out, positions, slots, q_weight, k_weight, eps) -> kvp_tokens:
+    first = q if q is not None else k
+    if first is None:
+        raise KvpError(1, "neither q nor k")
+    n = first.shape[0]
+    a = kvp_tokens()
+    a.struct_bytes, a.n_tokens, a.eps = ctypes.sizeof(kvp_tokens), n, eps
+    a.n_q_heads = q.shape[1] if q is not None and q.dim() == 3 else 0
+    a.n_kv_heads = k.shape[1] if k is not None and k.dim() == 3 else 0
+    for name, t, heads in (("q", q, 0), ("k", k, 0), ("v", v, a.n_kv_heads), ("q_out", q_out, a.n_q_heads), ("k_out", k_out, a.n_kv_heads)):
+        if t is None:
+            continue
+        at, s0, s1 = _rows(t, like, name, heads)
+        if t.shape[0] != n:
+            raise KvpError(1, f"{name}: {t.shape[0]} tokens, not {n}")
+        setattr(a, name, at)
+        stride = getattr(a, name + "_stride")
+        stride[0], stride[1] = s0, s1
+    a.positions = None if positions is None else _ints(positions, like[1], "positions", n)
+    a.slots = None if slots is None else _ints(slots, like[1], "slots", n)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            if w.dtype != like[0] or w.device != like[1] or tuple(w.shape) != (like[2],) or w.stride(0) != 1:
+                raise KvpError(1, f"{name}: {tuple(w.shape)} {w.dtype} on {w.device}")
+            setattr(a, name, w.data_ptr())
+    return a
+
+
+def norm_rope(q, k, positions, rope: Optional[Rope], q_out=None, k_out=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+              stream=None):
+    """``kvp_norm_rope``: q, k = [token][head][d] (either may be None) normed per head where there is a weight, then rotated to
+    ``positions`` [token]; what ``query_prefill`` takes."""
+    first = q if q is not None else k
+    if first is None or first.device.type != "cuda":
+        raise KvpError(1, "norm_rope: q or k on a CUDA device")
+    a = _tokens((first.dtype, first.device, first.shape[-1]), q, k, None, q_out, k_out, positions, None, q_weight, k_weight, eps)
+    _checked(lib().kvp_norm_rope(first.device.index, _dtype_of(first), first.shape[-1], ctypes.addressof(a),
+                                 rope.address if rope is not None else None, _raw_stream(first.device.index, stream)))
+
+
+class PagedCache:
+    """``kvp_cache`` over the caller's page tensors: ``k``, ``v`` = [layer][page][kv head][row][d] (order "heads") or
+    [layer][page][row][kv head][d] ("tokens"), with any strides.  CPU tensors make a host-only cache: pages are counted,
+    nothing runs."""
+
+    def __init__(self, k, v, n_q_heads: int, order: str = "heads", max_batch: int = 64, softmax_scale: float = 0.0):
+        import torch
+        self._L, self._h = lib(), ctypes.c_void_p()
+        if order not in ("heads", "tokens"):
+            raise KvpError(1, f"order {order!r} is neither 'heads' nor 'tokens'")
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+            raise KvpError(1, "k and v have to be alike, [layer][page][kv head][row][d] or [layer][page][row][kv head][d]")
+        if k.shape[4] > 1 and k.stride(4) != 1:
+            raise KvpError(1, "the elements of a row do not lie side by side")
+        head, row = (2, 3) if order == "heads" else (3, 2)
+        self.k, self.v, self.torch_device = k, v, k.device
+        self.device = k.device.index if k.device.type == "cuda" else -1
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape[0], k.shape[1], k.shape[head], k.shape[row], k.shape[4]
+        self.n_q_heads, self.max_batch = n_q_heads, max_batch
+        c = kvp_cache_config()
+        c.struct_bytes, c.device, c.n_layers, c.n_q_heads, c.n_kv_heads = ctypes.sizeof(c), self.device, self.n_layers, n_q_heads, self.n_kv_heads
+        c.head_dim, c.dtype, c.page_size, c.n_pages, c.max_batch = self.head_dim, _dtype_of(k), self.page_size, self.n_pages, max_batch
+        c.layer_stride, c.page_stride, c.head_stride, c.row_stride = k.stride(0), k.stride(1), k.stride(head), k.stride(row)
+        c.softmax_scale = softmax_scale
+        self.workspace = None
+        if self.device >= 0:
+            n = int(self._L.kvp_cache_workspace_bytes(ctypes.byref(c)))
+            self.workspace = torch.empty(n + 256, dtype=torch.uint8, device=k.device)
+            c.k, c.v = k.data_ptr(), v.data_ptr()
+            c.workspace, c.workspace_bytes = (self.workspace.data_ptr() + 255) // 256 * 256, n
+        self.cfg = c
+        _checked(self._L.kvp_cache_create(ctypes.byref(c), ctypes.byref(self._h)))
+        self._like = (k.dtype, k.device, self.head_dim)
+
+    def close(self):
+        if self._h:
+            self._L.kvp_cache_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc: int):
+        if rc != KVP_OK:
+            _checked(rc, self._h)
+
+    def _stream(self, stream):
+        return _raw_stream(self.device, stream) if self.device >= 0 else None
+
+    # -- rows ------------------------------------------------------------------------------------
+    def append(self, layer: int, k, v, positions, slots, rope: Optional[Rope] = None, q=None, q_out=None, k_out=None,
+               q_weight=None, k_weight=None, eps: float = 1e-6, stream=None):
+        """q, k, v = [token][head][d] as a layer's projections give them.  Keys (normed, rotated) and values go to ``slots``
+        [token] = page * page_size + row (a slot outside the store: nowhere), queries to ``q_out``."""
+        if k is None or v is None or slots is None:
+            raise KvpError(1, "append: k, v and slots are needed")
+        a = _tokens(self._like, q, k, v, q_out, k_out, positions, slots, q_weight, k_weight, eps)
+        self._check(self._L.kvp_cache_append(self._h, layer, ctypes.addressof(a), rope.address if rope is not None else None,
+                                             self._stream(stream)))
+
+    def attend(self, layer: int, q, table, lens, out, lse=None, first=None, stream=None):
+        """q, out = [request][q head][d]; table = [request][pages], lens, first = [request], int32; lse = float32
+        [request][q head].  Request b attends to its rows first[b] <= j < lens[b]."""
+        import torch
+        n = q.shape[0]
+        at, s0, s1 = _rows(q, self._like, "q", self.n_q_heads)
+        to, t0, t1 = _rows(out, self._like, "out", self.n_q_heads)
+        if out.shape[0] != n:
+            raise KvpError(1, f"out: {out.shape[0]} requests, not {n}")
+        if lse is not None and (lse.dtype != torch.float32 or lse.device != self.torch_device or tuple(lse.shape) != (n, self.n_q_heads) or not lse.is_contiguous()):
+            raise KvpError(1, f"lse: {tuple(lse.shape)} {lse.dtype} on {lse.device}")
+        dev = self.torch_device
+        self._check(self._L.kvp_cache_attend(
+            self._h, layer, n, at, struct.pack("2q", s0, s1), _ints(table, dev, "table", n, -1), table.stride(0), table.shape[1],
+            _ints(lens, dev, "lens", n), None if first is None else _ints(first, dev, "first", n), to, struct.pack("2q", t0, t1),
+            None if lse is None else lse.data_ptr(), self._stream(stream)))
+
+    def copy(self, src: Sequence[int], dst: Sequence[int], rows: Optional[Sequence[int]] = None, stream=None):
+        """The first rows[i] rows (None: all) of page src[i] to page dst[i], in all layers."""
+        if len(src) != len(dst) or (rows is not None and len(rows) != len(src)):
+            raise KvpError(1, "copy: lists of different lengths")
+        self._check(self._L.kvp_cache_copy(self._h, len(src), _i32_packed(src), _i32_packed(dst),
+                                           None if rows is None else _i32_packed(rows), self._stream(stream)))
+
+    def compact(self, table, lens, new_table, kept, n_kept, stream=None):
+        """Row i < n_kept[b] of new_table[b]'s pages becomes row kept[b][l][h][i] of table[b]'s; kept = [request][layer or
+        1][kv head or 1][entries], int32.  The new pages must not be among those that are read."""
+        n, dev = n_kept.shape[0], self.torch_device
+        at = _ints(kept, dev, "kept", n, -1, -1, -1)
+        if kept.shape[1] not in (1, self.n_layers) or kept.shape[2] not in (1, self.n_kv_heads):
+            raise KvpError(1, f"kept: lists for {kept.shape[1]} layers and {kept.shape[2]} heads")
+        strides = struct.pack("3q", kept.stride(0), kept.stride(1) if kept.shape[1] > 1 else 0, kept.stride(2) if kept.shape[2] > 1 else 0)
+        self._check(self._L.kvp_cache_compact(
+            self._h, n, _ints(table, dev, "table", n, -1), table.stride(0), table.shape[1], _ints(lens, dev, "lens", n),
+            _ints(new_table, dev, "new_table", n, -1), new_table.stride(0), new_table.shape[1], at, strides, kept.shape[3],
+            _ints(n_kept, dev, "n_kept", n), self._stream(stream)))
+
+    # -- pages -----------------------------------------------------------------------------------
+    def take(self, n: int) -> List[int]:
+        out = (ctypes.c_int32 * max(1, n))()
+        self._check(self._L.kvp_cache_take(self._h, n, out))
+        return list(out)[:n]
+
+    def share(self, pages: Sequence[int]):
+        self._check(self._L.kvp_cache_share(self._h, len(pages), _i32_packed(pages)))
+
+    def release(self, pages: Sequence[int]):
+        self._check(self._L.kvp_cache_release(self._h, len(pages), _i32_packed(pages)))
+
+    def fork(self, pages: Sequence[int], n_tokens: int, n_forks: int = 1, stream=None) -> List[List[int]]:
+        """``n_forks`` page lists for the first ``n_tokens`` rows of ``pages``: whole pages are shared, a last one that is not
+        full is copied to a new page for each."""
+        cols = -(-n_tokens // self.page_size)
+        if cols > len(pages):
+            raise KvpError(1, f"fork: {n_tokens} tokens in {len(pages)} pages of {self.page_size}")
+        out = (ctypes.c_int32 * max(1, n_forks * cols))()
+        self._check(self._L.kvp_cache_fork(self._h, n_tokens, _i32_packed(pages), n_forks, out, self._stream(stream)))
+        return [list(out[f * cols:(f + 1) * cols]) for f in range(n_forks)]
+
+    @property
+    def free_pages(self) -> int:
+        n = ctypes.c_int32(0)
+        self._check(self._L.kvp_cache_free_pages(self._h, ctypes.byref(n)))
+        return n.value

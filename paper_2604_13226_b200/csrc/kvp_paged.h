@@ -1,0 +1,66 @@
+// Declarations shared by the paged cache's host code (kvp_paged.cu) and its attention kernel (kvp_paged_attn.cu).
+#pragma once
+
+#include <string>
+#include <vector>
+
+#include "kvp_internal.h"
+
+// Quotient of a number n below 2^31 by a fixed divisor d, as a product and a shift: with l = ceil(log2 d) and
+// M = floor(2^(31+l) / d) + 1, M exceeds 2^(31+l) / d by at most 1, so n M / 2^(31+l) exceeds n / d by less than 2^-l <= 1 / d:
+// too little to reach the next whole number.
+struct kvp_divisor {
+    uint32_t mul;
+    int32_t shift;
+};
+
+// One layer of the store, or all of it (layer 0), as kernels see it; strides in bytes.
+struct kvp_store {
+    char *k, *v;
+    int64_t page_stride, head_stride, row_stride;
+    int32_t page_size, n_pages;
+    kvp_divisor by_page;
+};
+
+#ifdef __CUDACC__
+__device__ __forceinline__ int32_t divide(int32_t n, kvp_divisor d) { return (int32_t)(((uint64_t)(uint32_t)n * d.mul) >> d.shift); }
+#endif
+
+// Partial results of units whose rows several CTAs share, and a count of the parts that are in per unit.
+struct kvp_paged_ws {
+    float *part_o;             // [2 * CTAs][16][head_dim]
+    float2 *part_ml;           // [2 * CTAs][16]
+    int32_t *arrived;          // [units], zero between launches
+};
+
+struct kvp_paged_args {
+    kvp_store st;              // the layer's
+    const char *q;
+    char *out;
+    int64_t q_stride[2], out_stride[2];    // {request, head}, bytes
+    const int32_t *table, *lens, *first;
+    int64_t table_stride;
+    int32_t table_cols, batch, n_kv, group;
+    float *lse;
+    float scale;
+    kvp_paged_ws ws;
+};
+
+// Most and fewest query rows of a full unit (bf16, fp32); a group of more heads is several units.
+#define KVP_PAGED_ROWS 16
+#define KVP_PAGED_LEAST_ROWS 8
+int32_t kvp_paged_ctas(int32_t sm_count);
+cudaError_t kvp_paged_attn_prepare(int32_t dtype, int32_t head_dim);
+cudaError_t kvp_launch_paged_attn(const kvp_paged_args &a, int32_t dtype, int32_t head_dim, int32_t sm_count, cudaStream_t st);
+
+struct kvp_cache {
+    kvp_cache_config cfg;
+    int32_t elem_bytes, sm_count = 148;
+    float scale;
+    kvp_divisor by_page;
+    kvp_paged_ws ws = {};
+    std::vector<int32_t> holders;          // per page
+    std::vector<int32_t> free_pages;       // a stack: the lowest page on top at the start
+    std::vector<int32_t> scratch;          // per page, zero between calls
+    std::string err;
+};
