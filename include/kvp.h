@@ -519,12 +519,13 @@ KVP_API int32_t kvp_cache_append(kvp_cache *cache, int32_t layer, const kvp_toke
  * Attention of one new token per request over its rows first[b] <= j < lens[b] of `layer` (its own row among them, once
  * appended): softmax in fp32, q head h reads kv head h / (Hq/Hkv).
  *   q      device, {batch, head} strides in elements; out likewise.  16-byte aligned, strides multiples of 16 bytes
- *   table  device [batch][table_cols] with row stride table_stride: page numbers
+ *   table  device [batch][table_cols] with row stride table_stride: page numbers; n_kv_heads * batch * (table_cols *
+ *          page_size / 8 + 9), for groups of more than 8 heads once for each 8, is below 2^31
  *   lens, first   device [batch]; first may be NULL (0).  Lengths beyond table_cols pages end there.  A request without a
  *          row gets zeros and an lse of minus infinity
  *   lse    device float [batch][n_q_heads] or NULL
  * The work is shared out on the device, by the lengths that lie there when the kernel runs.
- * Errors: INVALID, CAPACITY (batch > max_batch), STATE (host only), CUDA.
+ * Errors: INVALID, CAPACITY (batch > max_batch, tables too large), STATE (host only), CUDA.
  */
 KVP_API int32_t kvp_cache_attend(kvp_cache *cache, int32_t layer, int32_t batch, const void *q, const int64_t *q_stride,
                          const int32_t *table, int64_t table_stride, int32_t table_cols, const int32_t *lens,

@@ -643,6 +643,8 @@ int32_t kvp_cache_attend(kvp_cache *c, int32_t layer, int32_t batch, const void 
             return fail(c, KVP_ERR_INVALID, "attend: rows of out overlap");
         if (llabs(table_stride) > (1ll << 56)) return fail(c, KVP_ERR_INVALID, "attend: table_stride");
     }
+    if (!kvp_paged_fits(batch, c->cfg.n_kv_heads, c->cfg.n_q_heads / c->cfg.n_kv_heads, std::min<int64_t>(INT32_MAX, (int64_t)table_cols * c->cfg.page_size)))
+        return fail(c, KVP_ERR_CAPACITY, "attend: tables of %d pages for %d requests", table_cols, batch);
     if (int32_t rc = check_runs(c, layer)) return rc;
     if (batch == 0) return KVP_OK;
     kvp_paged_args a;
@@ -657,7 +659,7 @@ int32_t kvp_cache_attend(kvp_cache *c, int32_t layer, int32_t batch, const void 
     a.lens = lens;
     a.first = first;
     a.table_stride = table_stride;
-    a.table_cols = table_cols;
+    a.room = (int32_t)std::min<int64_t>(INT32_MAX, (int64_t)table_cols * c->cfg.page_size);
     a.batch = batch;
     a.n_kv = c->cfg.n_kv_heads;
     a.group = c->cfg.n_q_heads / c->cfg.n_kv_heads;

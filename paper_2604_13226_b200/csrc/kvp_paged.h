@@ -40,7 +40,8 @@ struct kvp_paged_args {
     int64_t q_stride[2], out_stride[2];    // {request, head}, bytes
     const int32_t *table, *lens, *first;
     int64_t table_stride;
-    int32_t table_cols, batch, n_kv, group;
+    int32_t room;              // rows that a line of the table holds, INT32_MAX at most
+    int32_t batch, n_kv, group;
     float *lse;
     float scale;
     kvp_paged_ws ws;
@@ -50,6 +51,8 @@ struct kvp_paged_args {
 #define KVP_PAGED_ROWS 16
 #define KVP_PAGED_LEAST_ROWS 8
 int32_t kvp_paged_ctas(int32_t sm_count);
+// whether key tiles of a call (of 8 keys at least) can be counted in 31 bits, were all lists as long as `room`
+bool kvp_paged_fits(int64_t batch, int64_t n_kv, int64_t group, int64_t room);
 cudaError_t kvp_paged_attn_prepare(int32_t dtype, int32_t head_dim);
 cudaError_t kvp_launch_paged_attn(const kvp_paged_args &a, int32_t dtype, int32_t head_dim, int32_t sm_count, cudaStream_t st);
 

@@ -10,7 +10,7 @@
 //   lengths as they lie in device memory, so that a captured launch follows them.
 // * A unit inside one CTA is written out by it.  The parts of a unit that several CTAs share go to the workspace, and the CTA
 //   whose part is the last to arrive joins them, always in the order of the parts: results do not depend on who came last.
-// * Inside a CTA every warp streams key tiles of its own (warp w takes every 4th) through a ring of cp.async stages, without
+// * Inside a CTA every warp streams key tiles of its own (one in 4 or 8 of the CTA's) through a ring of cp.async stages, without
 //   any barrier; the warps' running maxima, sums and outputs are joined in shared memory at a unit's end.  The ring runs on
 //   into the next unit meanwhile.
 // * Rows are looked up one by one through the page table, by any page size; rows that are not there - behind the length, in
@@ -23,19 +23,24 @@
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kCtasPerSm = 2;
+constexpr int kWarpsPerSm = 8;             // in CTAs of 4 or of 8
 constexpr int kStages = 3;
 constexpr int kStageBytes = 8192;          // K and V rows of a tile
 constexpr int kUnitCost = 8;               // start and end of a unit, in key tiles of one warp
 constexpr int kMinShare = 8;               // tiles that a CTA is worth starting for
+constexpr int kJoin = 8;                   // parts that are read at once when a unit is joined
 
 template <typename T, int D> struct shape {
     static constexpr int kRowBytes = D * (int)sizeof(T);
     static constexpr int kWords = kRowBytes / 16;                      // 16-byte words of a row
     static constexpr int kKeys = kStageBytes / 2 / kRowBytes;          // keys of a tile
-    static constexpr int kSmemJoin = kWarps * 8 * D * 4;               // outputs of 8 rows of every warp
-    static constexpr int kSmem = kWarps * kStages * kStageBytes + kSmemJoin + kWarps * 8 * 8;
     static_assert(kKeys <= 32, "a lane looks up a row");
+};
+
+template <int D, int W> struct smem_layout {
+    static constexpr int kOut = W * kStages * kStageBytes;             // outputs of 8 rows of every warp, behind the rings
+    static constexpr int kMl = kOut + W * 8 * D * 4;                   // their maxima and sums
+    static constexpr int kBytes = kMl + W * 8 * 8;
 };
 
 __device__ __forceinline__ float exp2_fast(float x)
@@ -92,41 +97,45 @@ __device__ __forceinline__ float quad_sum(float x)
 // Visible rows of request b: [first, first + n).
 __device__ __forceinline__ int visible(const kvp_paged_args &a, int b, int &first)
 {
-    const int64_t room = (int64_t)a.table_cols * a.st.page_size;
-    int len = max(a.lens[b], 0);
+    const int len = min(max(a.lens[b], 0), a.room);
     first = a.first ? max(a.first[b], 0) : 0;
-    if (len > room) len = (int)room;
     return max(len - first, 0);
 }
 
-// Where on the line of all units a CTA's share lies, and a walk over the units that reach into it.
+// Where on the line of all units a CTA's share lies (the host has seen to it that the line is shorter than 2^31), and a walk
+// over the units that reach into it.
 struct line {
-    int64_t total, begin, end;
-    int ctas;
-    __device__ int64_t start(int cta) const { return total * cta / ctas; }
-    __device__ int owner(int64_t x) const { return (int)(((x + 1) * ctas - 1) / total); }
+    uint32_t share;
+    int begin, end;
+    __device__ int owner(int x) const { return (int)((uint32_t)x / share); }
+};
+
+struct piece {
+    int b, u, first, rows;                 // request, unit of the request, first visible row, visible rows
+    int lo, hi;                            // tiles; none for a unit without rows
+    int at;                                // where the unit begins on the line
 };
 
 template <int KEYS> struct walk {
-    int b, u, first, rows, tiles;          // the request, unit in it, its rows and tiles
-    int64_t at;                            // where the unit begins on the line
+    int b, u, first, rows, tiles;
+    int at;
     __device__ void request(const kvp_paged_args &a)
     {
         if (b >= a.batch) return;
         rows = visible(a, b, first);
         tiles = (rows + KEYS - 1) / KEYS;
     }
-    // To the next unit with something to do for this CTA: tiles [lo, hi), none for a unit without rows.  False: there is none.
-    __device__ bool next(const kvp_paged_args &a, const line &ln, int units, int &lo, int &hi, int &ub, int &uu, int &ufirst, int &urows, int64_t &uat)
+    // To the next unit with something to do for this CTA.  False: there is none.
+    __device__ bool next(const kvp_paged_args &a, const line &ln, int units, piece &p)
     {
         while (b < a.batch && at < ln.end) {
-            const int64_t t0 = at + kUnitCost;
-            lo = (int)max((int64_t)0, ln.begin - t0);
-            hi = (int)min((int64_t)tiles, ln.end - t0);
-            const bool mine = tiles == 0 ? at >= ln.begin : lo < hi;       // one without rows is its beginning's
-            if (tiles == 0) lo = hi = 0;
-            ub = b; uu = u; ufirst = first; urows = rows; uat = at;
-            at += kUnitCost + tiles;
+            const int t0 = at + kUnitCost;
+            p.lo = max(0, ln.begin - t0);
+            p.hi = min(tiles, ln.end - t0);
+            const bool mine = tiles == 0 ? at >= ln.begin : p.lo < p.hi;   // one without rows is its beginning's
+            if (tiles == 0) p.lo = p.hi = 0;
+            p.b = b; p.u = u; p.first = first; p.rows = rows; p.at = at;
+            at = t0 + tiles;
             if (++u == units) {
                 u = 0;
                 ++b;
@@ -138,100 +147,123 @@ template <int KEYS> struct walk {
     }
 };
 
-// Every warp for itself: 32 requests at a time.
-template <int KEYS>
-__device__ __forceinline__ void find_share(const kvp_paged_args &a, int units, line &ln, walk<KEYS> &w)
+// The lengths of all requests are added up by the whole CTA, a few requests per thread.  False: the CTA has no share.
+template <int KEYS, int W>
+__device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, line &ln, walk<KEYS> &w)
 {
-    const int lane = threadIdx.x % 32;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+    __shared__ int sums[W], found, found_at, found_len;
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    auto length = [&](int b) {                             // of one of a request's units
         int f;
-        if (b0 + lane < a.batch) total += (int64_t)units * (kUnitCost + (visible(a, b0 + lane, f) + KEYS - 1) / KEYS);
+        return (visible(a, b, f) + KEYS - 1) / KEYS + kUnitCost;
+    };
+    const int per = a.batch <= 32 * W ? 1 : (a.batch + 32 * W - 1) / (32 * W), b0 = threadIdx.x * per, b1 = min(b0 + per, a.batch);
+    int mine = 0;
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) mine += length(b) * units;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
     }
-    for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-    ln.total = total;
-    ln.ctas = (int)max((int64_t)1, min((int64_t)gridDim.x, total / kMinShare));
-    ln.begin = ln.end = 0;
-    if ((int)blockIdx.x >= ln.ctas) return;
-    ln.begin = ln.start(blockIdx.x);
-    ln.end = ln.start(blockIdx.x + 1);
-    int64_t before = 0;
-    for (int b0 = 0;; b0 += 32) {
-        int f, n = 0;
-        if (b0 + lane < a.batch) n = (visible(a, b0 + lane, f) + KEYS - 1) / KEYS + kUnitCost;
-        int64_t upto = (int64_t)n * units;                 // of this and the lanes in front
-        for (int o = 1; o < 32; o *= 2) {
-            const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
-        }
-        const unsigned past = __ballot_sync(0xffffffffu, before + upto > ln.begin);
-        if (past || b0 + 32 >= a.batch) {
-            const int who = past ? __ffs(past) - 1 : 31;
-            const int64_t base = before + __shfl_sync(0xffffffffu, upto - (int64_t)n * units, who);
-            const int len = __shfl_sync(0xffffffffu, n, who);
-            w.b = b0 + who;
-            w.u = len ? (int)((ln.begin - base) / len) : 0;
-            w.at = base + (int64_t)w.u * len;
-            w.request(a);
-            return;
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if (i < warp) upto += sums[i];
+        total += sums[i];
     }
+    const uint32_t ctas = max(1u, min(gridDim.x, (uint32_t)total / kMinShare));
+    ln.share = ((uint32_t)total + ctas - 1) / ctas;
+    if ((uint64_t)ln.share * blockIdx.x >= (uint32_t)total) return false;
+    ln.begin = (int)(ln.share * blockIdx.x);
+    ln.end = (int)min((uint32_t)total, ln.begin + ln.share);
+    if (upto - mine <= ln.begin && ln.begin < upto) {      // one thread has the request that the share begins in
+        int at = upto - mine;
+        for (int b = b0; b < b1; ++b) {
+            const int len = length(b);
+            if (ln.begin < at + len * units) {
+                found = b;
+                found_at = at;
+                found_len = len;
+                break;
+            }
+            at += len * units;
+        }
+    }
+    __syncthreads();
+    w.b = found;
+    w.u = (int)((uint32_t)(ln.begin - found_at) / (uint32_t)found_len);
+    w.at = found_at + w.u * found_len;
+    w.request(a);
+    return true;
 }
 
-// The tiles of a warp, one after the other, through the pieces of its CTA's share: what is loaded.
-template <typename T, int D> struct loader {
+// The tiles of a warp, one after the other, through the pieces of its CTA's share: what is loaded.  Pages are looked up two
+// tiles ahead, so that the table's latency is not in the way of the rows'.
+template <typename T, int D, int W> struct loader {
     using S = shape<T, D>;
     walk<S::kKeys> w;
-    int lo, hi, b, u, first, rows;         // the piece
-    int64_t at;
+    piece p;
     int tile, turn;                        // this warp's next tile; tiles of the CTA so far, modulo the warps
     bool more;
-    int page;                              // of this lane's row in that tile, -1: not there
-    int row;                               // and the row within it
+    struct place {
+        int page, row, head;               // of this lane's row in a tile; page -1: it is not there, -2: there is no tile
+    } next[2];
 
-    __device__ void piece(const kvp_paged_args &a, const line &ln, int units)
+    __device__ void start(const walk<S::kKeys> &from)
+    {
+        w = from;
+        turn = tile = p.hi = 0;
+        more = true;
+    }
+    __device__ void next_piece(const kvp_paged_args &a, const line &ln, int units)
     {
         const int warp = threadIdx.x / 32;
         while (more) {
-            more = w.next(a, ln, units, lo, hi, b, u, first, rows, at);
+            more = w.next(a, ln, units, p);
             if (!more) return;
-            const int n = max(hi - lo, 0), mine = lo + (warp + kWarps - turn) % kWarps;
-            turn = (turn + n) % kWarps;
-            if (mine < hi) {
+            const int mine = p.lo + (warp + W - turn) % W;
+            turn = (turn + p.hi - p.lo) % W;
+            if (mine < p.hi) {
                 tile = mine;
                 return;
             }
         }
     }
-    __device__ void look_up(const kvp_paged_args &a)
+    __device__ void look_up(const kvp_paged_args &a, const line &ln, int units, int row_tiles)
     {
-        page = -1;
+        next[0] = next[1];
+        place &x = next[1];
+        x.page = -2;
+        if (tile >= p.hi) next_piece(a, ln, units);
+        if (!more) return;
         const int lane = threadIdx.x % 32, i = tile * S::kKeys + lane;
-        if (!more || lane >= S::kKeys || i >= rows) return;
-        const int r = first + i, p = divide(r, a.st.by_page);
-        row = r - p * a.st.page_size;
-        page = a.table[b * a.table_stride + p];
-        if (page >= a.st.n_pages) page = -1;
+        x.page = -1;
+        if (lane < S::kKeys && i < p.rows) {
+            const int r = p.first + i, col = divide(r, a.st.by_page);
+            x.row = r - col * a.st.page_size;
+            x.head = p.u / row_tiles;
+            x.page = a.table[p.b * a.table_stride + col];
+            if (x.page < 0 || x.page >= a.st.n_pages) x.page = -1;
+        }
+        tile += W;
     }
-    __device__ void advance(const kvp_paged_args &a, const line &ln, int units)
+    // Copies the next tile to `stage` (shared address) and leaves which rows are there in *mask.
+    __device__ void issue(const kvp_paged_args &a, uint32_t stage, uint32_t *mask)
     {
-        tile += kWarps;
-        if (tile >= hi) piece(a, ln, units);
-        look_up(a);
-    }
-    // Copies the tile to `stage` (shared address) and leaves which rows are there in *mask; then on to the next tile.
-    __device__ void issue(const kvp_paged_args &a, const line &ln, int units, int row_tiles, uint32_t stage, uint32_t *mask)
-    {
-        if (more) {
+        const place x = next[0];
+        if (x.page != -2) {
             const int lane = threadIdx.x % 32;
-            const int64_t off = page < 0 ? 0 : page * a.st.page_stride + (u / row_tiles) * a.st.head_stride + row * a.st.row_stride;
-            const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+            const int64_t off = x.page < 0 ? 0 : x.page * a.st.page_stride + x.head * a.st.head_stride + x.row * a.st.row_stride;
+            const uint32_t there = __ballot_sync(0xffffffffu, x.page >= 0);
             if (lane == 0) *mask = there;
             constexpr int N = S::kKeys * S::kWords / 32;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int x = i * 32 + lane, r = x / S::kWords, c = x % S::kWords;
+                const int y = i * 32 + lane, r = y / S::kWords, c = y % S::kWords;
                 const int64_t o = __shfl_sync(0xffffffffu, off, r) + c * 16;
                 const bool in = (there >> r) & 1;
                 // bf16 rows are read by ldmatrix, eight rows at a time: the words of a row are permuted by its number
@@ -239,7 +271,6 @@ template <typename T, int D> struct loader {
                 copy16(to, a.st.k + o, in);
                 copy16(to + S::kKeys * S::kRowBytes, a.st.v + o, in);
             }
-            advance(a, ln, units);
         }
         copies_commit();
     }
@@ -249,7 +280,9 @@ template <typename T, int D> struct loader {
 
 // bf16: mma.sync m16n8k16, query rows as M.  With a group of at most 8 the lower half of M is free, and takes the rounding
 // remainders of the probabilities: P V with 16 bits of P in one instruction.  Wider groups take two.
+// fp32 units have 8 rows, those of a group of at most 4 the arithmetic of 4.
 template <typename T, int D, bool WIDE> struct tile_math;
+template <typename T> __host__ __device__ constexpr int unit_rows(bool wide) { return sizeof(T) == 2 ? (wide ? 16 : 8) : (wide ? 8 : 4); }
 
 template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
     using S = shape<__nv_bfloat16, D>;
@@ -258,7 +291,7 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
     float o[D / 8][4];
     float m[2], l[2];
 
-    __device__ void begin(const char *q0, int64_t head_stride, int n_rows)
+    __device__ void queries(const char *q0, int64_t head_stride, int n_rows)
     {
         const int g = threadIdx.x % 32 / 4, t = threadIdx.x % 4;
 #pragma unroll
@@ -271,6 +304,9 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
                 q[k][h + 2] = in ? *reinterpret_cast<const uint32_t *>(p + 16) : 0u;
             }
         }
+    }
+    __device__ void begin()
+    {
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.0f;
         m[0] = m[1] = -INFINITY;
@@ -387,15 +423,15 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
 };
 
 // fp32: FMA pipe.  Q K^T: 8 lanes share a key, each with a sixteenth or an eighth of its words, four keys at once; P V: a lane
-// has D/32 columns of every row.  8 query rows.
-template <int D> struct tile_math<float, D, false> {
+// has D/32 columns of every row.  4 query rows, or 8 (WIDE).
+template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
     using S = shape<float, D>;
-    static constexpr int R = 8, C = D / 32;
+    static constexpr int R = WIDE ? 8 : 4, C = D / 32;
     float q[R][D / 8];
     float o[R][C];
-    float m, l;                            // of row (lane % 8)
+    float m, l;                            // of row (lane % R)
 
-    __device__ void begin(const char *q0, int64_t head_stride, int n_rows)
+    __device__ void queries(const char *q0, int64_t head_stride, int n_rows)
     {
         const int part = threadIdx.x % 8;
 #pragma unroll
@@ -406,6 +442,9 @@ template <int D> struct tile_math<float, D, false> {
                 if (r < n_rows) x = *reinterpret_cast<const float4 *>(q0 + r * head_stride + (j * 8 + part) * 16);
                 q[r][4 * j] = x.x; q[r][4 * j + 1] = x.y; q[r][4 * j + 2] = x.z; q[r][4 * j + 3] = x.w;
             }
+    }
+    __device__ void begin()
+    {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -432,9 +471,13 @@ template <int D> struct tile_math<float, D, false> {
 #pragma unroll
                 for (int r = 0; r < R; ++r) x[r] += q[r][4 * j] * k.x + q[r][4 * j + 1] * k.y + q[r][4 * j + 2] * k.z + q[r][4 * j + 3] * k.w;
             }
-            // the 8 lanes of a key add up; lane `part` keeps row `part`
+            // the 8 lanes of a key add up; lane `part` keeps row `part % R`
+            if (R == 4) {
 #pragma unroll
-            for (int w = 4; w > 0; w /= 2)
+                for (int r = 0; r < R; ++r) x[r] += __shfl_xor_sync(0xffffffffu, x[r], 4);
+            }
+#pragma unroll
+            for (int w = R / 2; w > 0; w /= 2)
 #pragma unroll
                 for (int r = 0; r < w; ++r) {
                     const bool upper = part & w;
@@ -519,177 +562,226 @@ __device__ __forceinline__ void write_row(const kvp_paged_args &a, int b, int he
         a.lse[(int64_t)b * a.n_kv * a.group + head] = l > 0.0f ? (m + log2f(l)) * 0.693147180559945309f : (l == 0.0f ? -INFINITY : l);
 }
 
-template <typename T, int D, bool WIDE>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm)
+template <typename T, int D, bool WIDE, int W>
+__global__ void __launch_bounds__(32 * W, kWarpsPerSm / W)
 paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
 {
     using S = shape<T, D>;
     extern __shared__ __align__(128) char smem[];
-    __shared__ uint32_t masks[kWarps][kStages];
+    __shared__ uint32_t masks[W][kStages];
     __shared__ int last;
     pdl_launch_dependents();
     const int warp = threadIdx.x / 32;
-    constexpr int kUnitRows = sizeof(T) == 2 ? 16 : 8;
-    const int row_tiles = (a.group + kUnitRows - 1) / kUnitRows, units = a.n_kv * row_tiles;
+    constexpr int kUnitRows = unit_rows<T>(WIDE);
+    const int row_tiles = WIDE ? (a.group + kUnitRows - 1) / kUnitRows : 1, units = a.n_kv * row_tiles;
     const float scale = a.scale * 1.44269504088896341f;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * kStages * kStageBytes;
-    float *join_o = reinterpret_cast<float *>(smem + kWarps * kStages * kStageBytes);
-    float2 *join_ml = reinterpret_cast<float2 *>(smem + kWarps * kStages * kStageBytes + S::kSmemJoin);
+    float *join_o = reinterpret_cast<float *>(smem + smem_layout<D, W>::kOut);
+    float2 *join_ml = reinterpret_cast<float2 *>(smem + smem_layout<D, W>::kMl);
+    // parameters are fetched while the kernel in front ends
+    asm volatile("" ::"l"(a.lens), "l"(a.first), "l"(a.table), "l"(a.st.k), "l"(a.st.v), "l"(a.q), "r"(a.batch), "r"(a.room), "r"(units), "f"(scale));
     pdl_wait();
 
     line ln;
     walk<S::kKeys> w;
-    find_share<S::kKeys>(a, units, ln, w);
-    if ((int)blockIdx.x >= ln.ctas) return;
-    loader<T, D> ld;
-    ld.w = w;
-    ld.turn = 0;
-    ld.tile = ld.hi = 0;
-    ld.more = true;
-    ld.piece(a, ln, units);
-    ld.look_up(a);
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) ld.issue(a, ln, units, row_tiles, ring + s * kStageBytes, &masks[warp][s]);
+    if (!find_share<S::kKeys, W>(a, units, ln, w)) return;
+    // (Code is kept short here: a CTA of a short call runs most of it once, and instructions that are not in the cache take as
+    // long as the work.)
+    loader<T, D, W> ld;
+    ld.start(w);
+#pragma unroll 1
+    for (int s = -2; s < kStages - 1; ++s) {
+        if (s >= 0) ld.issue(a, ring + s * kStageBytes, &masks[warp][s]);
+        ld.look_up(a, ln, units, row_tiles);
+    }
 
     int stage = 0, turn = 0;
-    int lo, hi, b, u, first, rows;
-    int64_t at;
+    piece p = {}, p1;
     tile_math<T, D, WIDE> tm;
-    while (w.next(a, ln, units, lo, hi, b, u, first, rows, at)) {
-        const int h = u / row_tiles, head0 = h * a.group + u % row_tiles * kUnitRows;
-        const int n_rows = min(kUnitRows, a.group - u % row_tiles * kUnitRows);
-        tm.begin(a.q + b * a.q_stride[0] + head0 * a.q_stride[1], a.q_stride[1], n_rows);
-        for (int t = lo + (warp + kWarps - turn) % kWarps; t < hi; t += kWarps) {
+#pragma unroll 1
+    for (bool any = false;; any = true) {
+        // the next unit's queries are fetched while this one is joined
+        const bool more = w.next(a, ln, units, p1);
+        if (more) {
+            const int rt = p1.u % row_tiles * kUnitRows;
+            tm.queries(a.q + p1.b * a.q_stride[0] + (p1.u / row_tiles * a.group + rt) * a.q_stride[1], a.q_stride[1], min(kUnitRows, a.group - rt));
+        }
+        if (any) {
+            const int rt = p.u % row_tiles * kUnitRows, head0 = p.u / row_tiles * a.group + rt, n_rows = min(kUnitRows, a.group - rt);
+            [&]() {
+                // the warps' parts, 8 rows at a time; a thread has 4 columns of a row
+                const int tiles = (p.rows + S::kKeys - 1) / S::kKeys;
+                const bool whole = p.lo == 0 && p.hi == tiles;
+                const int slot = 2 * blockIdx.x + (p.lo > 0 ? 0 : 1);
+                for (int half = 0; half * 8 < n_rows; ++half) {
+                    tm.store(half, join_o + warp * 8 * D, join_ml + warp * 8);
+                    __syncthreads();
+                    for (int x = threadIdx.x; x < 8 * D / 4; x += 32 * W) {
+                        const int r = x / (D / 4), c4 = x % (D / 4);
+                        if (half * 8 + r >= n_rows) break;
+                        float m = -INFINITY;
+#pragma unroll
+                        for (int k = 0; k < W; ++k) m = fmaxf(m, join_ml[k * 8 + r].x);
+                        const float ref = m == -INFINITY ? 0.0f : m;
+                        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        float l = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < W; ++k) {
+                            const float2 ml = join_ml[k * 8 + r];
+                            const float f = exp2_fast(ml.x - ref);
+                            const float4 y = reinterpret_cast<const float4 *>(join_o + (k * 8 + r) * D)[c4];
+                            o.x += f * y.x; o.y += f * y.y; o.z += f * y.z; o.w += f * y.w;
+                            l += f * ml.y;
+                        }
+                        if (whole) {
+                            write_row<T, D>(a, p.b, head0 + half * 8 + r, c4, o, m, l);
+                        } else {
+                            const int to = slot * KVP_PAGED_ROWS + half * 8 + r;
+                            reinterpret_cast<float4 *>(a.ws.part_o + to * D)[c4] = o;
+                            if (c4 == 0) a.ws.part_ml[to] = make_float2(m, l);
+                        }
+                    }
+                    __syncthreads();
+                }
+                if (whole) return;
+
+                // whoever's part is the last joins them
+                const int t0 = p.at + kUnitCost;
+                const int c0 = ln.owner(t0), n_parts = ln.owner(t0 + tiles - 1) - c0 + 1;
+                int32_t *arrived = a.ws.arrived + p.b * units + p.u;
+                // (a barrier lies behind the parts' stores: thread 0's release covers all of them, and its acquire what others released)
+                if (threadIdx.x == 0) {
+                    int before;
+                    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(arrived) : "memory");
+                    last = before == n_parts - 1;
+                    if (last) *arrived = 0;
+                }
+                __syncthreads();
+                if (!last) return;
+                // D/4 threads take a row, four columns each; each of them first weighs one part, then all add up kJoin parts at a time
+                constexpr int L = D / 4;
+                for (int x = threadIdx.x; x - (int)threadIdx.x % 32 < n_rows * L; x += 32 * W) {
+                    const int r = min(x / L, n_rows - 1), c4 = x % L;
+                    const int row0 = 2 * c0 * KVP_PAGED_ROWS + r;          // of part p, p > 0: this + 2 p rows; of part 0 one slot on
+                    auto part = [&](int i) { return row0 + (i == 0 ? 1 : 2 * i) * KVP_PAGED_ROWS; };
+                    float m = -INFINITY, l = 0.0f;
+                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    for (int p0 = 0; p0 < n_parts; p0 += L) {
+                        const int n = min(L, n_parts - p0);
+                        const float2 ml = c4 < n ? __ldcg(a.ws.part_ml + part(p0 + c4)) : make_float2(-INFINITY, 0.0f);
+                        float weight = 0.0f;
+                        for (int k0 = 0; k0 < n; k0 += kJoin) {
+                            float4 y[kJoin];
+#pragma unroll
+                            for (int k = 0; k < kJoin; ++k) y[k] = __ldcg(reinterpret_cast<const float4 *>(a.ws.part_o + part(p0 + min(k0 + k, n - 1)) * D) + c4);
+                            if (k0 == 0) {
+                                float top = ml.x;
+#pragma unroll
+                                for (int w = L / 2; w > 0; w /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                                top = fmaxf(top, m);
+                                const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(m - ref);
+                                m = top;
+                                weight = exp2_fast(ml.x - ref);
+                                float sum = weight * ml.y;
+#pragma unroll
+                                for (int w = L / 2; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                                o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+                                l = l * f0 + sum;
+                            }
+#pragma unroll
+                            for (int k = 0; k < kJoin; ++k) {
+                                const float f = __shfl_sync(0xffffffffu, weight, (k0 + k) % L, L);
+                                if (k0 + k < n) { o.x += f * y[k].x; o.y += f * y[k].y; o.z += f * y[k].z; o.w += f * y[k].w; }
+                            }
+                        }
+                    }
+                    if (x < n_rows * L) write_row<T, D>(a, p.b, head0 + r, c4, o, m, l);
+                }
+            }();
+        }
+        if (!more) break;
+        p = p1;
+        tm.begin();
+#pragma unroll 1
+        for (int t = p.lo + (warp + W - turn) % W; t < p.hi; t += W) {
             copies_wait<kStages - 2>();
             __syncwarp();
             const int ahead = stage == 0 ? kStages - 1 : stage - 1;
             const uint32_t there = masks[warp][stage];
-            ld.issue(a, ln, units, row_tiles, ring + ahead * kStageBytes, &masks[warp][ahead]);
+            ld.issue(a, ring + ahead * kStageBytes, &masks[warp][ahead]);
+            ld.look_up(a, ln, units, row_tiles);
             tm.tile(ring + stage * kStageBytes, there, scale);
             stage = stage == kStages - 1 ? 0 : stage + 1;
         }
-        turn = (turn + max(hi - lo, 0)) % kWarps;
+        turn = (turn + p.hi - p.lo) % W;
         tm.end();
-
-        // the warps' parts, 8 rows at a time; a thread has 4 columns of a row
-        const int tiles = (rows + S::kKeys - 1) / S::kKeys;
-        const bool whole = lo <= 0 && hi >= tiles;
-        const int slot = 2 * blockIdx.x + (lo > 0 ? 0 : 1);
-        for (int half = 0; half * 8 < n_rows; ++half) {
-            tm.store(half, join_o + warp * 8 * D, join_ml + warp * 8);
-            __syncthreads();
-            for (int x = threadIdx.x; x < 8 * D / 4; x += kThreads) {
-                const int r = x / (D / 4), c4 = x % (D / 4);
-                if (half * 8 + r >= n_rows) break;
-                float m = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < kWarps; ++k) m = fmaxf(m, join_ml[k * 8 + r].x);
-                const float ref = m == -INFINITY ? 0.0f : m;
-                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                float l = 0.0f;
-#pragma unroll
-                for (int k = 0; k < kWarps; ++k) {
-                    const float2 ml = join_ml[k * 8 + r];
-                    const float f = exp2_fast(ml.x - ref);
-                    const float4 y = reinterpret_cast<const float4 *>(join_o + (k * 8 + r) * D)[c4];
-                    o.x += f * y.x; o.y += f * y.y; o.z += f * y.z; o.w += f * y.w;
-                    l += f * ml.y;
-                }
-                if (whole) {
-                    write_row<T, D>(a, b, head0 + half * 8 + r, c4, o, m, l);
-                } else {
-                    const int64_t p = (int64_t)slot * KVP_PAGED_ROWS + half * 8 + r;
-                    reinterpret_cast<float4 *>(a.ws.part_o + p * D)[c4] = o;
-                    if (c4 == 0) a.ws.part_ml[p] = make_float2(m, l);
-                }
-            }
-            __syncthreads();
-        }
-        if (whole) continue;
-
-        // whoever's part is the last joins them
-        const int64_t t0 = at + kUnitCost;
-        const int c0 = ln.owner(t0), n_parts = ln.owner(t0 + tiles - 1) - c0 + 1;
-        int32_t *arrived = a.ws.arrived + (int64_t)b * units + u;
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            last = atomicAdd(arrived, 1) == n_parts - 1;
-            if (last) *arrived = 0;
-        }
-        __syncthreads();
-        if (!last) continue;
-        __threadfence();
-        for (int x = threadIdx.x; x < n_rows * D / 4; x += kThreads) {
-            const int r = x / (D / 4), c4 = x % (D / 4);
-            float m = -INFINITY, l = 0.0f;
-            float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            for (int p0 = 0; p0 < n_parts; p0 += 4) {
-                float2 ml[4];
-                float4 y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int cta = c0 + p0 + k;
-                    const int64_t p = (int64_t)(2 * cta + (p0 + k == 0 ? 1 : 0)) * KVP_PAGED_ROWS + r;
-                    ml[k] = make_float2(-INFINITY, 0.0f);
-                    y[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (p0 + k < n_parts) {
-                        ml[k] = __ldcg(a.ws.part_ml + p);
-                        y[k] = __ldcg(reinterpret_cast<const float4 *>(a.ws.part_o + p * D) + c4);
-                    }
-                }
-                float top = m;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top = fmaxf(top, ml[k].x);
-                const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(m - ref);
-                m = top;
-                o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
-                l *= f0;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float f = exp2_fast(ml[k].x - ref);
-                    o.x += f * y[k].x; o.y += f * y[k].y; o.z += f * y[k].z; o.w += f * y[k].w;
-                    l += f * ml[k].y;
-                }
-            }
-            write_row<T, D>(a, b, head0 + r, c4, o, m, l);
-        }
     }
     copies_wait<0>();
 }
 
-template <typename T, int D, bool WIDE>
-cudaError_t launch(const kvp_paged_args &a, int sm_count, cudaStream_t st)
+template <typename T, int D, bool WIDE, int W>
+cudaError_t launch(const kvp_paged_args &a, int64_t units, int sm_count, cudaStream_t st)
 {
     // no more CTAs than the longest lists that the tables can hold are worth
-    constexpr int kUnitRows = sizeof(T) == 2 ? 16 : 8;
-    const int64_t units = (int64_t)a.batch * a.n_kv * ((a.group + kUnitRows - 1) / kUnitRows);
-    const int64_t tiles = ((int64_t)a.table_cols * a.st.page_size + shape<T, D>::kKeys - 1) / shape<T, D>::kKeys;
-    const int64_t most = std::min<int64_t>(sm_count * kCtasPerSm, units * std::min<int64_t>(tiles + kUnitCost, 1 << 24) / kMinShare);
-    return launch_pdl(paged_attn_kernel<T, D, WIDE>, dim3((unsigned)std::max<int64_t>(1, most)), dim3(kThreads), shape<T, D>::kSmem, st, a);
+    const int64_t tiles = (a.room + (int64_t)shape<T, D>::kKeys - 1) / shape<T, D>::kKeys;
+    const int64_t most = std::min<int64_t>(sm_count * (kWarpsPerSm / W), units * (tiles + kUnitCost) / kMinShare);
+    return launch_pdl(paged_attn_kernel<T, D, WIDE, W>, dim3((unsigned)std::max<int64_t>(1, most)), dim3(32 * W), smem_layout<D, W>::kBytes, st, a);
 }
 
 template <typename T, int D, bool WIDE>
-cudaError_t prepare()
+cudaError_t launch_any(const kvp_paged_args &a, int sm_count, cudaStream_t st)
 {
-    return cudaFuncSetAttribute(paged_attn_kernel<T, D, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, shape<T, D>::kSmem);
+    constexpr int kUnitRows = unit_rows<T>(WIDE);
+    const int64_t units = (int64_t)a.batch * a.n_kv * ((a.group + kUnitRows - 1) / kUnitRows);
+    const int64_t tiles = units * ((a.room + (int64_t)shape<T, D>::kKeys - 1) / shape<T, D>::kKeys);
+    if (tiles + units * kUnitCost > INT32_MAX) return cudaErrorInvalidValue;       // kvp_paged_fits
+    // CTAs of 8 warps, one per SM, halve the parts that a unit is joined from: 8 x 8,000 rows of one kv head with 16 query heads
+    // 27 -> 20 us, 133,120 rows 92.5 -> 90.0.  CTAs of 4 join within themselves more cheaply and hide one another's ends: 256 x
+    // 200 rows 64 -> 48 us, 2,785 rows 9.7 -> 9.1, 16 x 16,000 rows of fp32 heads of 64 92 -> 86.  The lengths are not known
+    // here; tables for long lists mean long ones.
+    const bool eight = units < 2 * sm_count && (WIDE || (sizeof(T) == 2 && tiles >= 200ll * sm_count));
+    return eight ? launch<T, D, WIDE, 8>(a, units, sm_count, st) : launch<T, D, WIDE, 4>(a, units, sm_count, st);
+}
+
+template <typename T, int D, bool WIDE, int W> cudaError_t prepare_one()
+{
+    return cudaFuncSetAttribute(paged_attn_kernel<T, D, WIDE, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_layout<D, W>::kBytes);
+}
+template <typename T, int D, bool WIDE> cudaError_t prepare()
+{
+    const cudaError_t e = prepare_one<T, D, WIDE, 4>();
+    return e != cudaSuccess ? e : prepare_one<T, D, WIDE, 8>();
 }
 
 }  // namespace
 
-int32_t kvp_paged_ctas(int32_t sm_count) { return sm_count * kCtasPerSm; }
+bool kvp_paged_fits(int64_t batch, int64_t n_kv, int64_t group, int64_t room)
+{
+    return (double)batch * n_kv * ((group + KVP_PAGED_LEAST_ROWS - 1) / KVP_PAGED_LEAST_ROWS) * ((room + 7) / 8 + kUnitCost) <= INT32_MAX;
+}
+
+int32_t kvp_paged_ctas(int32_t sm_count) { return sm_count * kWarpsPerSm / 4; }
 
 cudaError_t kvp_paged_attn_prepare(int32_t dtype, int32_t head_dim)
 {
-    if (dtype == KVP_DTYPE_F32) return head_dim == 128 ? prepare<float, 128, false>() : prepare<float, 64, false>();
-    const cudaError_t e = head_dim == 128 ? prepare<__nv_bfloat16, 128, false>() : prepare<__nv_bfloat16, 64, false>();
-    if (e != cudaSuccess) return e;
-    return head_dim == 128 ? prepare<__nv_bfloat16, 128, true>() : prepare<__nv_bfloat16, 64, true>();
+    cudaError_t e;
+    if (dtype == KVP_DTYPE_F32) {
+        e = head_dim == 128 ? prepare<float, 128, false>() : prepare<float, 64, false>();
+        return e != cudaSuccess ? e : head_dim == 128 ? prepare<float, 128, true>() : prepare<float, 64, true>();
+    }
+    e = head_dim == 128 ? prepare<__nv_bfloat16, 128, false>() : prepare<__nv_bfloat16, 64, false>();
+    return e != cudaSuccess ? e : head_dim == 128 ? prepare<__nv_bfloat16, 128, true>() : prepare<__nv_bfloat16, 64, true>();
+}
+
+template <typename T>
+static cudaError_t launch_paged(const kvp_paged_args &a, int32_t head_dim, int32_t sm_count, cudaStream_t st)
+{
+    if (a.group <= unit_rows<T>(false))
+        return head_dim == 128 ? launch_any<T, 128, false>(a, sm_count, st) : launch_any<T, 64, false>(a, sm_count, st);
+    return head_dim == 128 ? launch_any<T, 128, true>(a, sm_count, st) : launch_any<T, 64, true>(a, sm_count, st);
 }
 
 cudaError_t kvp_launch_paged_attn(const kvp_paged_args &a, int32_t dtype, int32_t head_dim, int32_t sm_count, cudaStream_t st)
 {
-    if (dtype == KVP_DTYPE_F32) return head_dim == 128 ? launch<float, 128, false>(a, sm_count, st) : launch<float, 64, false>(a, sm_count, st);
-    if (a.group <= 8) return head_dim == 128 ? launch<__nv_bfloat16, 128, false>(a, sm_count, st) : launch<__nv_bfloat16, 64, false>(a, sm_count, st);
-    return head_dim == 128 ? launch<__nv_bfloat16, 128, true>(a, sm_count, st) : launch<__nv_bfloat16, 64, true>(a, sm_count, st);
+    return dtype == KVP_DTYPE_F32 ? launch_paged<float>(a, head_dim, sm_count, st) : launch_paged<__nv_bfloat16>(a, head_dim, sm_count, st);
 }

@@ -214,16 +214,19 @@ def test_norm_rope_arguments():
 
 
 def test_rope_arguments():
+    for kw in (dict(rotary_dim=24), dict(rotary_dim=-16), dict(pairing=2), dict(theta=0.0), dict(theta=math.inf), dict(scale=0.5), dict(scale=0.0),
+               dict(scale=math.nan), dict(magnitude=0.0), dict(magnitude=math.inf), dict(original_positions=-1.0),
+               dict(original_positions=8192, low_rotations=4.0, high_rotations=4.0), dict(inv_freq=[math.nan] * 32), dict(inv_freq=[1.0] * 31)):
+        refused(INVALID, kvp.Rope, 64, **kw)
     k = torch.zeros(3, 2, 64)
     i = torch.zeros(3, dtype=torch.int32)
-    c = cache()
-    for r in (kvp.Rope(64, rotary_dim=24), kvp.Rope(64, rotary_dim=80), kvp.Rope(64, rotary_dim=-16), kvp.Rope(64, pairing=2), kvp.Rope(64, theta=0.0),
-              kvp.Rope(64, theta=math.inf), kvp.Rope(64, scale=0.5), kvp.Rope(64, scale=math.nan), kvp.Rope(64, magnitude=0.0),
-              kvp.Rope(64, original_positions=-1.0), kvp.Rope(64, original_positions=8192, low_rotations=4.0, high_rotations=4.0),
-              kvp.Rope(64, inv_freq=[math.nan] * 32)):
-        refused(INVALID, c.append, 0, k, k, i, i, rope=r)
-    refused(INVALID, kvp.Rope, 64, inv_freq=[1.0] * 31)
-    refused(INVALID, kvp.Rope(64, scale=0.0).frequencies)
+    refused(INVALID, cache().append, 0, k, k, i, i, rope=kvp.Rope(64, rotary_dim=80))       # more than a head has
+    r = kvp.Rope(64)
+    r.struct.struct_bytes = 8
+    refused(INVALID, cache().append, 0, k, k, i, i, rope=r)
+    r = kvp.Rope(64)
+    r.struct.reserved = 1
+    refused(INVALID, cache().append, 0, k, k, i, i, rope=r)
 
 
 @pytest.mark.parametrize("r,theta,scale,original,low,high", [(128, 500000.0, 8.0, 8192, 1.0, 4.0), (64, 10000.0, 4.0, 32768, 1.0, 32.0),
