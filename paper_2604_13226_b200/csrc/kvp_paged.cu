@@ -13,170 +13,335 @@
 
 namespace {
 
+// Two fp32 numbers in a register pair, and the packed arithmetic on them.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi)
+{
+    f32x2 x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
+    return x;
+}
+__device__ __forceinline__ void unpack2(f32x2 x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+
+// A 16-byte word of elements as pairs of fp32 numbers, and back (rounded to nearest).
 template <typename T> struct elem;
 template <> struct elem<float> {
     static constexpr int kPerVec = 4;
-    __device__ static float get(float x) { return x; }
-    __device__ static float put(float x) { return x; }
+    __device__ static void get(uint4 u, f32x2 (&x)[2])
+    {
+        x[0] = (f32x2)u.y << 32 | u.x;
+        x[1] = (f32x2)u.w << 32 | u.z;
+    }
+    __device__ static uint4 put(const f32x2 (&x)[2]) { return make_uint4((uint32_t)x[0], (uint32_t)(x[0] >> 32), (uint32_t)x[1], (uint32_t)(x[1] >> 32)); }
+    __device__ static float one(float x) { return x; }
 };
 template <> struct elem<__nv_bfloat16> {
     static constexpr int kPerVec = 8;
-    __device__ static float get(__nv_bfloat16 x) { return __bfloat162float(x); }
-    __device__ static __nv_bfloat16 put(float x) { return __float2bfloat16_rn(x); }
-};
-template <typename T> union vec16 {
-    uint4 u;
-    T e[elem<T>::kPerVec];
+    __device__ static f32x2 wide(uint32_t w) { return (f32x2)(w & 0xffff0000u) << 32 | (w << 16); }
+    __device__ static uint32_t narrow(f32x2 x)
+    {
+        float lo, hi;
+        unpack2(x, lo, hi);
+        uint32_t w;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+        return w;
+    }
+    __device__ static void get(uint4 u, f32x2 (&x)[4])
+    {
+        x[0] = wide(u.x); x[1] = wide(u.y); x[2] = wide(u.z); x[3] = wide(u.w);
+    }
+    __device__ static uint4 put(const f32x2 (&x)[4]) { return make_uint4(narrow(x[0]), narrow(x[1]), narrow(x[2]), narrow(x[3])); }
+    __device__ static float one(__nv_bfloat16 x) { return __bfloat162float(x); }
 };
 
 // ---- norms, rotation, append ----------------------------------------------------------------------------------
 
-constexpr int kTokens = 4;         // most tokens of a block
-
+struct rows_at {
+    const char *p;
+    int64_t stride[2];             // {token, head}, bytes
+};
 struct append_args {
-    const char *q, *k, *v;
-    char *q_out, *k_out;
-    int64_t q_stride[2], k_stride[2], v_stride[2], q_out_stride[2], k_out_stride[2];   // {token, head}, bytes
+    rows_at q, k, v, q_out, k_out;
     const int32_t *positions, *slots;
     const char *q_weight, *k_weight;
     kvp_store st;                  // st.k null: no pages
     int32_t n_tokens, n_q, n_k, n_v;   // heads of each that there is something to do for
-    int32_t tokens, rows;          // per block: tokens, and rows of a token (all, or a part of them)
     int32_t rotary, pairing;
     float eps, magnitude;
     double turns[64];              // f_i / 2 pi
 };
 
-// A row is one head of one token.  A thread takes two 16-byte words of it that are each other's rotation partners (half
-// layout; the words behind rotary_dim in pairs as they come), so that neither layout needs an exchange between threads and
-// the sum of squares takes log2(words/2) shuffles.  The angle is formed in double precision, as a part of a turn, and its
-// sine and cosine from the rounded remainder: |remainder| <= 1/2 turn, so the rounding moves the angle by 2^-25 turns at
-// most, wherever the position lies.
-template <typename T, int D>
-__global__ void __launch_bounds__(256)
-append_tokens_kernel(const __grid_constant__ append_args a)
-{
-    constexpr int EV = elem<T>::kPerVec, V = D / EV, L = V / 2, RP = 256 / L;     // words of a row, threads of a row, rows at once
-    __shared__ __align__(16) float2 cs[kTokens][D / 2];
-    pdl_launch_dependents();
-    const int t0 = blockIdx.x * a.tokens, n_t = min(a.tokens, a.n_tokens - t0), half_rot = a.rotary / 2;
-    const int tt = threadIdx.x / 64, ti = threadIdx.x % 64;
-    pdl_wait();
-    if (tt < n_t && ti < half_rot) {
-        const double turn = (double)a.positions[t0 + tt] * a.turns[ti];
-        float s, c;
-        sincospif(2.0f * (float)(turn - rint(turn)), &s, &c);
-        cs[tt][ti] = make_float2(a.magnitude * c, a.magnitude * s);
+// A row is one head of one token.  A thread takes two 16-byte words of it that are each other's rotation partners (half layout),
+// so that neither layout needs an exchange between threads and a sum of squares takes log2(words / 2) shuffles.  A warp takes
+// a token, or a part of its heads: the token's angles are formed once, and the sines, cosines and weights that a thread needs
+// stay in its registers for all heads (read from shared memory for each head they took twice the wavefronts of the rows
+// themselves).  The angle is formed in double precision, as a part of a turn, and its sine and cosine from the rounded
+// remainder: |remainder| <= 1/2 turn, so the rounding moves the angle by 2^-25 turns at most, wherever the position lies.
+template <typename T, int D> struct row_math {
+    static constexpr int EV = elem<T>::kPerVec, P = EV / 2, L = D / EV / 2, R = 32 / L;   // elements and pairs of a word, threads of a row, rows of a warp
+    int w0, w1;                            // the words
+    bool turns;
+    f32x2 c[P], s[P];                      // of this thread's pairs: the half layout's P pairs, or P / 2 of each word
+    f32x2 gx[P], gy[P];                    // weights
+
+    __device__ row_math(int rotary)
+    {
+        const int j = threadIdx.x % L, half = rotary / EV / 2;             // half: words of one half of the rotated part
+        turns = j < half;
+        w0 = turns ? j : half + j;
+        w1 = w0 + (turns ? half : L - half);
     }
-    __syncthreads();
-    const int j = threadIdx.x % L, lane_row = threadIdx.x / L;
-    const int half = a.rotary / EV / 2;                                            // words of one half of the rotated part
-    const bool turns = j < half;
-    const int w0 = turns ? j : 2 * half + 2 * (j - half), w1 = turns ? j + half : w0 + 1;
-    const int rows = a.n_q + a.n_k + a.n_v, r0 = blockIdx.y * a.rows, n_rows = min(a.rows, rows - r0);
-    for (int w = lane_row; w - lane_row < n_t * n_rows; w += RP) {
-        const bool in = w < n_t * n_rows;
-        const int t = t0 + (in ? w / n_rows : 0), tl = t - t0, r = in ? r0 + w % n_rows : r0;
-        const int kind = r < a.n_q ? 0 : r < a.n_q + a.n_k ? 1 : 2;
-        const int head = kind == 0 ? r : kind == 1 ? r - a.n_q : r - a.n_q - a.n_k;
-        const char *src = kind == 0 ? a.q + t * a.q_stride[0] + head * a.q_stride[1]
-                        : kind == 1 ? a.k + t * a.k_stride[0] + head * a.k_stride[1]
-                                    : a.v + t * a.v_stride[0] + head * a.v_stride[1];
-        vec16<T> x, y;
-        x.u = reinterpret_cast<const uint4 *>(src)[w0];
-        y.u = reinterpret_cast<const uint4 *>(src)[w1];
-        const char *weight = kind == 0 ? a.q_weight : kind == 1 ? a.k_weight : nullptr;
-        float fx[EV], fy[EV];
-        float ss = 0.0f;
+    __device__ void weigh(const char *weight)
+    {
+        elem<T>::get(reinterpret_cast<const uint4 *>(weight)[w0], gx);
+        elem<T>::get(reinterpret_cast<const uint4 *>(weight)[w1], gy);
+    }
+    // norms: whether any row of the warp is normed (the same for all its threads)
+    __device__ void row(uint4 &x, uint4 &y, bool norms, bool norm, bool rotate, float eps, int pairing) const
+    {
+        f32x2 fx[P], fy[P];
+        elem<T>::get(x, fx);
+        elem<T>::get(y, fy);
+        float inv = 1.0f;
+        if (norms) {
+            f32x2 sum = 0;
 #pragma unroll
-        for (int e = 0; e < EV; ++e) {
-            fx[e] = elem<T>::get(x.e[e]);
-            fy[e] = elem<T>::get(y.e[e]);
-            ss += fx[e] * fx[e] + fy[e] * fy[e];
-        }
-        if (a.q_weight || a.k_weight) {
+            for (int e = 0; e < P; ++e) sum = fma2(fy[e], fy[e], fma2(fx[e], fx[e], sum));
+            float ss, hi;
+            unpack2(sum, ss, hi);
+            ss += hi;
 #pragma unroll
             for (int o = L / 2; o > 0; o /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            inv = rsqrtf(ss * (1.0f / D) + eps);
         }
-        if (weight) {
-            const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
-            vec16<T> gx, gy;
-            gx.u = reinterpret_cast<const uint4 *>(weight)[w0];
-            gy.u = reinterpret_cast<const uint4 *>(weight)[w1];
+        if (norm) {
+            const f32x2 inv2 = pack2(inv, inv);
 #pragma unroll
-            for (int e = 0; e < EV; ++e) {
-                fx[e] *= inv * elem<T>::get(gx.e[e]);
-                fy[e] *= inv * elem<T>::get(gy.e[e]);
+            for (int e = 0; e < P; ++e) {
+                fx[e] = mul2(mul2(fx[e], gx[e]), inv2);
+                fy[e] = mul2(mul2(fy[e], gy[e]), inv2);
             }
         }
-        if (kind < 2 && turns) {
-            if (a.pairing == 0) {
+        if (turns && rotate) {
+            if (pairing == 0) {
+                const f32x2 minus = pack2(-1.0f, -1.0f);
 #pragma unroll
-                for (int e = 0; e < EV; ++e) {
-                    const float2 c = cs[tl][w0 * EV + e];
-                    const float p = fx[e], q = fy[e];
-                    fx[e] = p * c.x - q * c.y;
-                    fy[e] = p * c.y + q * c.x;
+                for (int e = 0; e < P; ++e) {
+                    const f32x2 p = fx[e], q = fy[e];
+                    fx[e] = fma2(p, c[e], mul2(mul2(q, s[e]), minus));
+                    fy[e] = fma2(q, c[e], mul2(p, s[e]));
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < EV; e += 2) {
-                    float2 c = cs[tl][(w0 * EV + e) / 2];
-                    float p = fx[e], q = fx[e + 1];
-                    fx[e] = p * c.x - q * c.y;
-                    fx[e + 1] = p * c.y + q * c.x;
-                    c = cs[tl][(w1 * EV + e) / 2];
-                    p = fy[e];
-                    q = fy[e + 1];
-                    fy[e] = p * c.x - q * c.y;
-                    fy[e + 1] = p * c.y + q * c.x;
+                for (int e = 0; e < P; ++e) {
+                    float c0, c1, s0, s1, p, q;
+                    unpack2(c[e], c0, c1);
+                    unpack2(s[e], s0, s1);
+                    unpack2(fx[e], p, q);
+                    fx[e] = pack2(p * c0 - q * s0, p * s0 + q * c0);
+                    unpack2(fy[e], p, q);
+                    fy[e] = pack2(p * c1 - q * s1, p * s1 + q * c1);
                 }
             }
         }
-        if (kind < 2) {
+        x = elem<T>::put(fx);
+        y = elem<T>::put(fy);
+    }
+};
+
+__device__ __forceinline__ uint4 *words_at(const rows_at &r, int token, int head)
+{
+    return reinterpret_cast<uint4 *>(const_cast<char *>(r.p) + token * r.stride[0] + head * r.stride[1]);
+}
+
+// A token's row in the pages.
+struct page_row {
+    char *k, *v;                   // null: nowhere
+    __device__ page_row(const append_args &a, int token) : k(nullptr), v(nullptr)
+    {
+        if (!a.st.k) return;
+        const int32_t slot = a.slots[token];
+        if (slot < 0 || slot >= a.st.n_pages * a.st.page_size) return;
+        const int32_t page = divide(slot, a.st.by_page), row = slot - page * a.st.page_size;
+        const int64_t at = page * a.st.page_stride + row * a.st.row_stride;
+        k = a.st.k + at;
+        v = a.st.v + at;
+    }
+};
+
+// The pairs of a thread, from a table of (cosine, sine): half layout, elements 2e and 2e + 1 of both words; the other, pair e of
+// the first and of the second word.
+template <typename T, int D>
+__device__ __forceinline__ void take_angles(row_math<T, D> &m, const float2 *table, int pairing)
+{
+    constexpr int P = row_math<T, D>::P;
 #pragma unroll
-            for (int e = 0; e < EV; ++e) {
-                x.e[e] = elem<T>::put(fx[e]);
-                y.e[e] = elem<T>::put(fy[e]);
+    for (int e = 0; e < P; ++e) {
+        const int i0 = !m.turns ? 0 : pairing == 0 ? m.w0 * 2 * P + 2 * e : m.w0 * P + e, i1 = !m.turns ? 0 : pairing == 0 ? i0 + 1 : m.w1 * P + e;
+        const float2 t0 = table[i0], t1 = table[i1];
+        m.c[e] = pack2(t0.x, t1.x);
+        m.s[e] = pack2(t0.y, t1.y);
+    }
+}
+
+__device__ __forceinline__ float2 angle_of(int position, double turns, float magnitude)
+{
+    const double turn = (double)position * turns;
+    float sine, cosine;
+    sincospif(2.0f * (float)(turn - rint(turn)), &sine, &cosine);
+    return make_float2(magnitude * cosine, magnitude * sine);
+}
+
+// Many tokens: bound by DRAM.  A thread has four rows under way; blocks take tokens in turn, so that the frequencies are fetched
+// once (a token per warp and launch: 33,280 tokens 141 us, in turn 133; in one wave 131, but 8,000 tokens 73 instead of 64).
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 2)
+append_many_kernel(const __grid_constant__ append_args a)
+{
+    typedef row_math<T, D> math;
+    constexpr int R = math::R, U = 4;
+    __shared__ float2 turned_by[8][D / 2];                 // (cosine, sine)
+    pdl_launch_dependents();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, mine = lane / math::L;
+    math m(a.rotary);
+    double f[D / 64];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) f[i] = lane + 32 * i < a.rotary / 2 ? a.turns[lane + 32 * i] : 0.0;
+    pdl_wait();
+    for (int token = blockIdx.x * 8 + warp; token < a.n_tokens; token += gridDim.x * 8) {
+        uint4 x[U], y[U];
+        auto fetch = [&](const rows_at &r, int u, int head, int end) {
+            if (head >= end) return;
+            const uint4 *p = words_at(r, token, head);
+            x[u] = p[m.w0];
+            y[u] = p[m.w1];
+        };
+        auto store = [&](uint4 *p, int u) {
+            p[m.w0] = x[u];
+            p[m.w1] = y[u];
+        };
+        const int position = a.rotary ? a.positions[token] : 0;
+        const page_row to(a, token);
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(a.q, u, mine + u * R, a.n_q);
+        if (a.rotary) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) turned_by[warp][lane + 32 * i] = angle_of(position, f[i], a.magnitude);
+            __syncwarp();
+            take_angles<T, D>(m, turned_by[warp], a.pairing);
+        }
+        if (a.q_weight) m.weigh(a.q_weight);
+        for (int h0 = 0; h0 < a.n_q; h0 += U * R) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int head = h0 + u * R + mine;
+                if (head - mine >= a.n_q) break;
+                m.row(x[u], y[u], a.q_weight, a.q_weight, true, a.eps, a.pairing);
+                if (head < a.n_q) store(words_at(a.q_out, token, head), u);
             }
+#pragma unroll
+            for (int u = 0; u < U; ++u) fetch(a.q, u, h0 + (U + u) * R + mine, a.n_q);
         }
-        if (!in) continue;
-        char *out = kind == 0 ? a.q_out + t * a.q_out_stride[0] + head * a.q_out_stride[1]
-                  : kind == 1 && a.k_out ? a.k_out + t * a.k_out_stride[0] + head * a.k_out_stride[1] : nullptr;
-        if (out) {
-            reinterpret_cast<uint4 *>(out)[w0] = x.u;
-            reinterpret_cast<uint4 *>(out)[w1] = y.u;
-        }
-        if (kind > 0 && a.st.k) {
-            const int32_t slot = a.slots[t];
-            if (slot >= 0 && slot < a.st.n_pages * a.st.page_size) {
-                const int32_t page = divide(slot, a.st.by_page), row = slot - page * a.st.page_size;
-                char *to = (kind == 1 ? a.st.k : a.st.v) + page * a.st.page_stride + head * a.st.head_stride + row * a.st.row_stride;
-                reinterpret_cast<uint4 *>(to)[w0] = x.u;
-                reinterpret_cast<uint4 *>(to)[w1] = y.u;
+        if (a.k_weight) m.weigh(a.k_weight);
+        for (int h0 = 0; h0 < max(a.n_k, a.n_v); h0 += U / 2 * R) {
+#pragma unroll
+            for (int u = 0; u < U / 2; ++u) {
+                fetch(a.k, u, h0 + u * R + mine, a.n_k);
+                fetch(a.v, U / 2 + u, h0 + u * R + mine, a.n_v);
+            }
+#pragma unroll
+            for (int u = 0; u < U / 2; ++u) {
+                const int head = h0 + u * R + mine;
+                if (head - mine < a.n_k) m.row(x[u], y[u], a.k_weight, a.k_weight, true, a.eps, a.pairing);
+                if (head < a.n_k && a.k_out.p) store(words_at(a.k_out, token, head), u);
+                if (head < a.n_k && to.k) store(reinterpret_cast<uint4 *>(to.k + head * a.st.head_stride), u);
+                if (head < a.n_v && to.v) store(reinterpret_cast<uint4 *>(to.v + head * a.st.head_stride), U / 2 + u);
             }
         }
     }
 }
 
-template <typename T>
-cudaError_t launch_append(append_args &a, int head_dim, int sm_count, cudaStream_t st)
+// Few tokens: latency.  A block has as many rows of one token (q heads, then k, then v) as it has threads for, and forms the
+// angles while they are fetched.
+template <typename T, int D>
+__global__ void __launch_bounds__(256, 4)
+append_few_kernel(const __grid_constant__ append_args a)
 {
-    const int at_once = 256 / (head_dim / elem<T>::kPerVec / 2), rows = a.n_q + a.n_k + a.n_v;
-    // Few tokens: one pass of a block each, rows of a token spread over blocks; many: four tokens a block, so that every thread
-    // forms an angle.
-    int64_t parts = 1;
-    if (a.n_tokens >= 8 * sm_count) {
-        a.tokens = kTokens;
-        a.rows = rows;
-    } else {
-        a.tokens = 1;
-        a.rows = std::min(rows, at_once);
-        parts = (rows + a.rows - 1) / a.rows;
+    typedef row_math<T, D> math;
+    __shared__ float2 turned_by[D / 2];
+    pdl_launch_dependents();
+    math m(a.rotary);
+    const int token = blockIdx.x, n_qk = a.n_q + a.n_k, r = blockIdx.y * (256 / math::L) + threadIdx.x / math::L;
+    const int kind = r < a.n_q ? 0 : r < n_qk ? 1 : r < n_qk + a.n_v ? 2 : 3, head = kind == 0 ? r : kind == 1 ? r - a.n_q : r - n_qk;   // q, k, v, nothing
+    const double f = (int)threadIdx.x < a.rotary / 2 ? a.turns[threadIdx.x] : 0.0;
+    pdl_wait();
+    uint4 x = make_uint4(0, 0, 0, 0), y = x;
+    if (kind < 3) {
+        const uint4 *p = words_at(kind == 0 ? a.q : kind == 1 ? a.k : a.v, token, head);
+        x = p[m.w0];
+        y = p[m.w1];
     }
-    const dim3 grid((a.n_tokens + a.tokens - 1) / a.tokens, (unsigned)parts);
-    return head_dim == 128 ? launch_pdl(append_tokens_kernel<T, 128>, grid, dim3(256), 0, st, a)
-                           : launch_pdl(append_tokens_kernel<T, 64>, grid, dim3(256), 0, st, a);
+    const bool norm = (kind == 0 && a.q_weight) || (kind == 1 && a.k_weight);
+    if (norm) m.weigh(kind == 0 ? a.q_weight : a.k_weight);
+    if ((int)threadIdx.x < a.rotary / 2) turned_by[threadIdx.x] = angle_of(a.positions[token], f, a.magnitude);
+    __syncthreads();
+    if (a.rotary) take_angles<T, D>(m, turned_by, a.pairing);
+    if (__any_sync(0xffffffffu, kind < 2)) {
+        uint4 x1 = x, y1 = y;
+        m.row(x1, y1, a.q_weight || a.k_weight, norm, a.rotary > 0, a.eps, a.pairing);
+        if (kind < 2) {
+            x = x1;
+            y = y1;
+        }
+    }
+    auto store = [&](uint4 *p) {
+        p[m.w0] = x;
+        p[m.w1] = y;
+    };
+    if (kind == 0) store(words_at(a.q_out, token, head));
+    if (kind == 1 && a.k_out.p) store(words_at(a.k_out, token, head));
+    if (kind == 1 || kind == 2) {
+        const page_row to(a, token);
+        if (to.k) store(reinterpret_cast<uint4 *>((kind == 1 ? to.k : to.v) + head * a.st.head_stride));
+    }
+}
+
+kvp_divisor divisor(int32_t d)
+{
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    return {(uint32_t)((1ull << (31 + l)) / (uint64_t)d + 1), 31 + l};
+}
+
+template <typename T, int D>
+cudaError_t launch_append(append_args &a, int sm_count, cudaStream_t st)
+{
+    // 512 tokens of 32/8 heads: 7.1 us as many, 5.9 as few; 1,000 of 28/4: 8.8, 11.4.  Twice as many blocks as fit, so that the
+    // last ones even out.
+    if (a.n_tokens >= 4 * sm_count)
+        return launch_pdl(append_many_kernel<T, D>, dim3(std::min((a.n_tokens + 7) / 8, 4 * sm_count)), dim3(256), 0, st, a);
+    const int rows = a.n_q + a.n_k + a.n_v, at_once = 256 / row_math<T, D>::L;
+    return launch_pdl(append_few_kernel<T, D>, dim3(a.n_tokens, (rows + at_once - 1) / at_once), dim3(256), 0, st, a);
+}
+
+cudaError_t launch_append(append_args &a, int32_t dtype, int32_t head_dim, int sm_count, cudaStream_t st)
+{
+    if (dtype == KVP_DTYPE_BF16)
+        return head_dim == 128 ? launch_append<__nv_bfloat16, 128>(a, sm_count, st) : launch_append<__nv_bfloat16, 64>(a, sm_count, st);
+    return head_dim == 128 ? launch_append<float, 128>(a, sm_count, st) : launch_append<float, 64>(a, sm_count, st);
 }
 
 // ---- copies of pages --------------------------------------------------------------------------------------------
@@ -229,15 +394,18 @@ struct compact_args {
     int64_t layer_stride;
     const int32_t *table, *lens, *new_table, *kept, *n_kept;
     int64_t table_stride, new_stride, kept_stride[3];
-    int32_t table_cols, new_cols, max_kept, n_kv, words;
+    int32_t table_cols, new_cols, max_kept, n_kv;
 };
 
-constexpr int kCompactRows = 64;
+constexpr int kCompactRows = 32, kCompactVecs = 4;         // rows of a block; words in flight per thread
 
-// Block (64 new rows, layer and head, request): where each row comes from and goes to is looked up once, then the words of K
-// and V are moved.
-__global__ void __launch_bounds__(256)
-compact_kernel(const compact_args a)
+// Block (kCompactRows new rows, layer and head, request): where each row comes from and goes to is looked up once, then the
+// words of K and V are moved.  Bound by DRAM; the look-ups, three round trips, hide behind other blocks, so blocks are small and
+// many: 4 x 8,000-10,560 rows to two fifths, 8 layers, 64 rows and 8 words a thread (4 blocks per SM) 168 us, 64 and 4 (8
+// blocks) 163, 32 and 4 161 = 6.4 TB/s.
+template <int WORDS>
+__global__ void __launch_bounds__(256, 8)
+compact_kernel(const __grid_constant__ compact_args a)
 {
     __shared__ int64_t from[kCompactRows], to[kCompactRows];
     pdl_launch_dependents();
@@ -246,14 +414,14 @@ compact_kernel(const compact_args a)
     const int n = min(min(a.n_kept[b], a.max_kept) - i0, kCompactRows);
     if (n <= 0) return;
     if ((int)threadIdx.x < n) {
-        const int i = i0 + threadIdx.x;
+        const int i = i0 + threadIdx.x, new_page = divide(i, a.st.by_page);
+        const int dst = new_page < a.new_cols ? a.new_table[b * a.new_stride + new_page] : -1;
         const int row = a.kept[b * a.kept_stride[0] + layer * a.kept_stride[1] + h * a.kept_stride[2] + i];
         const int64_t base = layer * a.layer_stride + h * a.st.head_stride;
         int64_t f = -1, t = -1;
-        const int new_page = divide(i, a.st.by_page);
-        if (row >= 0 && row < a.lens[b] && new_page < a.new_cols) {
+        if (row >= 0 && row < a.lens[b]) {
             const int page = divide(row, a.st.by_page);
-            const int src = page < a.table_cols ? a.table[b * a.table_stride + page] : -1, dst = a.new_table[b * a.new_stride + new_page];
+            const int src = page < a.table_cols ? a.table[b * a.table_stride + page] : -1;
             if (src >= 0 && src < a.st.n_pages && dst >= 0 && dst < a.st.n_pages) {
                 f = base + src * a.st.page_stride + (row - page * a.st.page_size) * a.st.row_stride;
                 t = base + dst * a.st.page_stride + (i - new_page * a.st.page_size) * a.st.row_stride;
@@ -263,24 +431,27 @@ compact_kernel(const compact_args a)
         to[threadIdx.x] = t;
     }
     __syncthreads();
-    const int n_words = 2 * n * a.words;                   // K and V of a row in turn
-    for (int w0 = threadIdx.x; w0 < n_words; w0 += 256 * kCopyVecs) {
-        uint4 x[kCopyVecs];
+    // K and V of a row in turn
+    for (int w0 = threadIdx.x; w0 < 2 * WORDS * n; w0 += 256 * kCompactVecs) {
+        uint4 x[kCompactVecs];
 #pragma unroll
-        for (int u = 0; u < kCopyVecs; ++u) {
-            const int w = w0 + 256 * u;
-            if (w >= n_words) break;
-            const int r = w / (2 * a.words), c = w % (2 * a.words);
-            if (from[r] >= 0) x[u] = *reinterpret_cast<const uint4 *>((c < a.words ? a.st.k : a.st.v) + from[r] + (c % a.words) * 16);
+        for (int u = 0; u < kCompactVecs; ++u) {
+            const int w = w0 + 256 * u, r = w / (2 * WORDS), c = w % (2 * WORDS);
+            if (r < n && from[r] >= 0) x[u] = *reinterpret_cast<const uint4 *>((c < WORDS ? a.st.k : a.st.v) + from[r] + c % WORDS * 16);
         }
 #pragma unroll
-        for (int u = 0; u < kCopyVecs; ++u) {
-            const int w = w0 + 256 * u;
-            if (w >= n_words) break;
-            const int r = w / (2 * a.words), c = w % (2 * a.words);
-            if (from[r] >= 0) *reinterpret_cast<uint4 *>((c < a.words ? a.st.k : a.st.v) + to[r] + (c % a.words) * 16) = x[u];
+        for (int u = 0; u < kCompactVecs; ++u) {
+            const int w = w0 + 256 * u, r = w / (2 * WORDS), c = w % (2 * WORDS);
+            if (r < n && from[r] >= 0) *reinterpret_cast<uint4 *>((c < WORDS ? a.st.k : a.st.v) + to[r] + c % WORDS * 16) = x[u];
         }
     }
+}
+
+cudaError_t launch_compact(const compact_args &a, int words, int n_layers, int batch, cudaStream_t st)
+{
+    const dim3 grid((unsigned)(((int64_t)a.max_kept + kCompactRows - 1) / kCompactRows), (unsigned)(n_layers * a.n_kv), (unsigned)batch);
+    return words == 8 ? launch_pdl(compact_kernel<8>, grid, dim3(256), 0, st, a)
+         : words == 16 ? launch_pdl(compact_kernel<16>, grid, dim3(256), 0, st, a) : launch_pdl(compact_kernel<32>, grid, dim3(256), 0, st, a);
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
@@ -320,13 +491,6 @@ struct on_device {
     }
     ~on_device() { if (before >= 0) (void)cudaSetDevice(before); }
 };
-
-kvp_divisor divisor(int32_t d)
-{
-    int l = 0;
-    while ((1ll << l) < d) ++l;
-    return {(uint32_t)((1ull << (31 + l)) / (uint64_t)d + 1), 31 + l};
-}
 
 bool odd16(const void *p) { return ((uintptr_t)p & 15) != 0; }
 
@@ -418,17 +582,17 @@ int32_t token_args(kvp_cache *c, const kvp_tokens *t, const kvp_rope *rope, int3
     if (turned && !t->positions) return fail(c, KVP_ERR_INVALID, "tokens: a rotation needs positions");
     if (((uintptr_t)t->positions | (uintptr_t)t->slots) & 3) return fail(c, KVP_ERR_INVALID, "tokens: positions and slots must be aligned");
     if (odd16(t->q_weight) || odd16(t->k_weight)) return fail(c, KVP_ERR_INVALID, "tokens: weights must be 16-byte aligned");
-    const struct { const void *p; const int64_t *s; int64_t *to; int32_t heads; } x[5] = {
-        {t->q, t->q_stride, a.q_stride, t->n_q_heads}, {t->k, t->k_stride, a.k_stride, t->n_kv_heads}, {t->v, t->v_stride, a.v_stride, t->n_kv_heads},
-        {t->q_out, t->q_out_stride, a.q_out_stride, t->n_q_heads}, {t->k_out, t->k_out_stride, a.k_out_stride, t->n_kv_heads}};
+    const struct { const void *p; const int64_t *s; rows_at &to; int32_t heads; } x[5] = {
+        {t->q, t->q_stride, a.q, t->n_q_heads}, {t->k, t->k_stride, a.k, t->n_kv_heads}, {t->v, t->v_stride, a.v, t->n_kv_heads},
+        {t->q_out, t->q_out_stride, a.q_out, t->n_q_heads}, {t->k_out, t->k_out_stride, a.k_out, t->n_kv_heads}};
     for (int i = 0; i < 5; ++i) {
-        x[i].to[0] = x[i].to[1] = 0;
+        x[i].to = {(const char *)x[i].p, {0, 0}};
         if (!x[i].p) continue;
         if (odd16(x[i].p)) return fail(c, KVP_ERR_INVALID, "tokens: pointers must be 16-byte aligned");
         for (int k = 0; k < 2; ++k) {
             if (x[i].s[k] < -(1ll << 56) || x[i].s[k] > (1ll << 56) || x[i].s[k] * e % 16)
                 return fail(c, KVP_ERR_INVALID, "tokens: strides must be multiples of 16 bytes");
-            x[i].to[k] = x[i].s[k] * e;
+            x[i].to.stride[k] = x[i].s[k] * e;
         }
         // rows that are written must not lie over one another
         if (i >= 3 && ((t->n_tokens > 1 && llabs(x[i].s[0]) < head_dim) || (x[i].heads > 1 && llabs(x[i].s[1]) < head_dim)))
@@ -438,11 +602,6 @@ int32_t token_args(kvp_cache *c, const kvp_tokens *t, const kvp_rope *rope, int3
     if ((t->q && t->q_out == t->q && (t->q_stride[0] != t->q_out_stride[0] || t->q_stride[1] != t->q_out_stride[1])) ||
         (t->k && t->k_out == t->k && (t->k_stride[0] != t->k_out_stride[0] || t->k_stride[1] != t->k_out_stride[1])))
         return fail(c, KVP_ERR_INVALID, "tokens: in place with other strides");
-    a.q = (const char *)t->q;
-    a.k = (const char *)t->k;
-    a.v = (const char *)t->v;
-    a.q_out = (char *)t->q_out;
-    a.k_out = (char *)t->k_out;
     a.positions = t->positions;
     a.slots = t->slots;
     a.q_weight = (const char *)t->q_weight;
@@ -543,8 +702,7 @@ int32_t kvp_norm_rope(int32_t device, int32_t dtype, int32_t head_dim, const kvp
     int sms = 0;
     cudaError_t e = dev.rc;
     if (e == cudaSuccess) e = sms_of(device, &sms);
-    if (e == cudaSuccess) e = dtype == KVP_DTYPE_BF16 ? launch_append<__nv_bfloat16>(a, head_dim, sms, (cudaStream_t)stream)
-                                                      : launch_append<float>(a, head_dim, sms, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = launch_append(a, dtype, head_dim, sms, (cudaStream_t)stream);
     return e == cudaSuccess ? (int32_t)KVP_OK : cuda_failed(nullptr, "norm_rope", e);
 }
 
@@ -620,8 +778,7 @@ int32_t kvp_cache_append(kvp_cache *c, int32_t layer, const kvp_tokens *tokens, 
     a.st = store_of(c, layer);
     on_device dev(c->cfg.device);
     cudaError_t e = dev.rc;
-    if (e == cudaSuccess) e = c->cfg.dtype == KVP_DTYPE_BF16 ? launch_append<__nv_bfloat16>(a, c->cfg.head_dim, c->sm_count, (cudaStream_t)stream)
-                                                             : launch_append<float>(a, c->cfg.head_dim, c->sm_count, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = launch_append(a, c->cfg.dtype, c->cfg.head_dim, c->sm_count, (cudaStream_t)stream);
     return e == cudaSuccess ? (int32_t)KVP_OK : cuda_failed(c, "append", e);
 }
 
@@ -726,11 +883,9 @@ int32_t kvp_cache_compact(kvp_cache *c, int32_t batch, const int32_t *table, int
     a.new_cols = new_cols;
     a.max_kept = max_kept;
     a.n_kv = c->cfg.n_kv_heads;
-    a.words = c->cfg.head_dim * c->elem_bytes / 16;
     on_device dev(c->cfg.device);
     cudaError_t e = dev.rc;
-    const dim3 grid((unsigned)(((int64_t)max_kept + kCompactRows - 1) / kCompactRows), (unsigned)(c->cfg.n_layers * c->cfg.n_kv_heads), (unsigned)batch);
-    if (e == cudaSuccess) e = launch_pdl(compact_kernel, grid, dim3(256), 0, (cudaStream_t)stream, a);
+    if (e == cudaSuccess) e = launch_compact(a, c->cfg.head_dim * c->elem_bytes / 16, c->cfg.n_layers, batch, (cudaStream_t)stream);
     return e == cudaSuccess ? (int32_t)KVP_OK : cuda_failed(c, "compact", e);
 }
 
