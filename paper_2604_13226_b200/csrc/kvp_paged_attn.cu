@@ -26,9 +26,9 @@ namespace {
 constexpr int kWarpsPerSm = 8;             // in CTAs of 4 or of 8
 constexpr int kStages = 3;
 constexpr int kStageBytes = 8192;          // K and V rows of a tile
-constexpr int kUnitCost = 8;               // start and end of a unit, in key tiles of one warp
+constexpr int kUnitCost = 16;              // start and end of a unit, in key tiles of one warp
 constexpr int kMinShare = 8;               // tiles that a CTA is worth starting for
-constexpr int kJoin = 8;                   // parts that are read at once when a unit is joined
+constexpr int kJoin = 8;                    // parts that are read at once when a unit is joined
 
 template <typename T, int D> struct shape {
     static constexpr int kRowBytes = D * (int)sizeof(T);
@@ -147,7 +147,7 @@ template <int KEYS> struct walk {
     }
 };
 
-// The lengths of all requests are added up by the whole CTA, a few requests per thread.  False: the CTA has no share.
+// The lengths of more than 32 requests are added up by the whole CTA, a few requests per thread.  False: the CTA has no share.
 template <int KEYS, int W>
 __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, line &ln, walk<KEYS> &w)
 {
@@ -157,16 +157,38 @@ __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, l
         int f;
         return (visible(a, b, f) + KEYS - 1) / KEYS + kUnitCost;
     };
+    auto cut = [&](int total) {                            // this CTA's share of the line
+        const uint32_t ctas = max(1u, min(gridDim.x, (uint32_t)total / kMinShare));
+        ln.share = ((uint32_t)total + ctas - 1) / ctas;
+        if ((uint64_t)ln.share * blockIdx.x >= (uint32_t)total) return false;
+        ln.begin = (int)(ln.share * blockIdx.x);
+        ln.end = (int)min((uint32_t)total, ln.begin + ln.share);
+        return true;
+    };
+    auto scan = [&](int n) {                               // of the lanes up to this one
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int x = __shfl_up_sync(0xffffffffu, n, o);
+            if (lane >= o) n += x;
+        }
+        return n;
+    };
+    if (a.batch <= 32) {                                   // every warp for itself: no barrier on the way to the first rows
+        const int len = lane < a.batch ? length(lane) : 0, upto = scan(len * units);
+        if (!cut(__shfl_sync(0xffffffffu, upto, 31))) return false;
+        const int who = __ffs(__ballot_sync(0xffffffffu, ln.begin < upto)) - 1;
+        const int at = __shfl_sync(0xffffffffu, upto - len * units, who), one = __shfl_sync(0xffffffffu, len, who);
+        w.b = who;
+        w.u = (int)((uint32_t)(ln.begin - at) / (uint32_t)one);
+        w.at = at + w.u * one;
+        w.request(a);
+        return true;
+    }
     const int per = a.batch <= 32 * W ? 1 : (a.batch + 32 * W - 1) / (32 * W), b0 = threadIdx.x * per, b1 = min(b0 + per, a.batch);
     int mine = 0;
 #pragma unroll 4
     for (int b = b0; b < b1; ++b) mine += length(b) * units;
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-    }
+    int upto = scan(mine);
     if (lane == 31) sums[warp] = upto;
     __syncthreads();
     int total = 0;
@@ -175,11 +197,7 @@ __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, l
         if (i < warp) upto += sums[i];
         total += sums[i];
     }
-    const uint32_t ctas = max(1u, min(gridDim.x, (uint32_t)total / kMinShare));
-    ln.share = ((uint32_t)total + ctas - 1) / ctas;
-    if ((uint64_t)ln.share * blockIdx.x >= (uint32_t)total) return false;
-    ln.begin = (int)(ln.share * blockIdx.x);
-    ln.end = (int)min((uint32_t)total, ln.begin + ln.share);
+    if (!cut(total)) return false;
     if (upto - mine <= ln.begin && ln.begin < upto) {      // one thread has the request that the share begins in
         int at = upto - mine;
         for (int b = b0; b < b1; ++b) {
@@ -275,6 +293,10 @@ template <typename T, int D, int W> struct loader {
         copies_commit();
     }
 };
+
+// Where column c of row r of a warp's part lies: the eight rows that a warp writes at once are permuted against one another by
+// 32 bytes, else they would all fall on the same banks.
+template <int D> __device__ __forceinline__ int join_at(int r, int c) { return r * D + ((c / 8) ^ r) * 8 + c % 8; }
 
 // ---- the arithmetic of a warp ---------------------------------------------------------------------------------------
 
@@ -407,16 +429,17 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) l[h] = quad_sum(l[h]);
     }
-    // rows [8 half, 8 half + 8) of this warp to shared memory: out [8][D], ml [8]
-    __device__ void store(int half, float *out, float2 *ml)
+    // rows [8 half, 8 half + n), n <= 8, of this warp to shared memory: out [n][D], ml [n]
+    __device__ void store(int half, int n, float *out, float2 *ml)
     {
         const int g = threadIdx.x % 32 / 4, t = threadIdx.x % 4;
+        if (g >= n) return;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
             float2 x;
             if (WIDE) x = half == 0 ? make_float2(o[i][0], o[i][1]) : make_float2(o[i][2], o[i][3]);
             else x = make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]);
-            *reinterpret_cast<float2 *>(out + g * D + i * 8 + t * 2) = x;
+            *reinterpret_cast<float2 *>(out + join_at<D>(g, i * 8 + t * 2)) = x;
         }
         if (t == 0) ml[g] = make_float2(m[WIDE ? half : 0], l[WIDE ? half : 0]);
     }
@@ -531,14 +554,17 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
         l += __shfl_xor_sync(0xffffffffu, l, 8);
         l += __shfl_xor_sync(0xffffffffu, l, 16);
     }
-    __device__ void store(int, float *out, float2 *ml)
+    __device__ void store(int, int n, float *out, float2 *ml)
     {
         const int lane = threadIdx.x % 32;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int c = 0; c < C; ++c) out[r * D + lane * C + c] = o[r][c];
-        if (lane < R) ml[lane] = make_float2(m, l);
+        for (int r = 0; r < R; ++r) {
+            if (r >= n) break;
+            float *to = out + join_at<D>(r, lane * C);
+            if (C == 4) *reinterpret_cast<float4 *>(to) = make_float4(o[r][0], o[r][1], o[r][C - 2], o[r][C - 1]);
+            else *reinterpret_cast<float2 *>(to) = make_float2(o[r][0], o[r][1]);
+        }
+        if (lane < n) ml[lane] = make_float2(m, l);
     }
 };
 
@@ -595,7 +621,7 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
         ld.look_up(a, ln, units, row_tiles);
     }
 
-    int stage = 0, turn = 0;
+    int stage = 0, turn = 0, flip = 0;
     piece p = {}, p1;
     tile_math<T, D, WIDE> tm;
 #pragma unroll 1
@@ -613,23 +639,27 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
                 const int tiles = (p.rows + S::kKeys - 1) / S::kKeys;
                 const bool whole = p.lo == 0 && p.hi == tiles;
                 const int slot = 2 * blockIdx.x + (p.lo > 0 ? 0 : 1);
+                // (groups of up to four, whose units are all alike, take the two halves of the space in turn, and need no barrier
+                // behind them: the next unit's lies in front of the one after)
+                const bool alternate = !WIDE && n_rows <= 4;
+                const int base = alternate ? (flip ^= 4) : 0;
                 for (int half = 0; half * 8 < n_rows; ++half) {
-                    tm.store(half, join_o + warp * 8 * D, join_ml + warp * 8);
+                    tm.store(half, min(8, n_rows - half * 8), join_o + (warp * 8 + base) * D, join_ml + warp * 8 + base);
                     __syncthreads();
                     for (int x = threadIdx.x; x < 8 * D / 4; x += 32 * W) {
                         const int r = x / (D / 4), c4 = x % (D / 4);
                         if (half * 8 + r >= n_rows) break;
                         float m = -INFINITY;
 #pragma unroll
-                        for (int k = 0; k < W; ++k) m = fmaxf(m, join_ml[k * 8 + r].x);
+                        for (int k = 0; k < W; ++k) m = fmaxf(m, join_ml[k * 8 + base + r].x);
                         const float ref = m == -INFINITY ? 0.0f : m;
                         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                         float l = 0.0f;
 #pragma unroll
                         for (int k = 0; k < W; ++k) {
-                            const float2 ml = join_ml[k * 8 + r];
+                            const float2 ml = join_ml[k * 8 + base + r];
                             const float f = exp2_fast(ml.x - ref);
-                            const float4 y = reinterpret_cast<const float4 *>(join_o + (k * 8 + r) * D)[c4];
+                            const float4 y = *reinterpret_cast<const float4 *>(join_o + (k * 8 + base) * D + join_at<D>(r, c4 * 4));
                             o.x += f * y.x; o.y += f * y.y; o.z += f * y.z; o.w += f * y.w;
                             l += f * ml.y;
                         }
@@ -641,7 +671,7 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
                             if (c4 == 0) a.ws.part_ml[to] = make_float2(m, l);
                         }
                     }
-                    __syncthreads();
+                    if (!alternate || !whole) __syncthreads();
                 }
                 if (whole) return;
 
