@@ -493,7 +493,8 @@ typedef struct kvp_cache_config {
     int32_t page_size;          /* rows of a page, >= 1; page_size * n_kv_heads <= 2^24               */
     int32_t n_pages;            /* n_pages * page_size < 2^31                                         */
     int32_t max_batch;          /* requests of one kvp_cache_attend                                   */
-    int64_t layer_stride, page_stride, head_stride, row_stride;   /* elements; multiples of 16 bytes  */
+    int64_t layer_stride, page_stride, head_stride, row_stride;   /* elements; multiples of 16 bytes; the rows of a
+                                   layer lie within 2^32 times the largest power of two that divides the last three */
     double softmax_scale;       /* 0 -> 1/sqrt(head_dim)                                              */
     void *k, *v;                /* device, 16-byte aligned                                            */
     void *workspace;            /* device, 256-byte aligned                                           */
@@ -503,9 +504,11 @@ typedef struct kvp_cache_config {
 /* Workspace size that the configuration needs.  0 if cfg is invalid. */
 KVP_API uint64_t kvp_cache_workspace_bytes(const kvp_cache_config *cfg);
 
-/* k, v and the workspace are borrowed; the workspace's counters are zeroed here (synchronised before return).
-   Errors: INVALID, CAPACITY (workspace too small), CUDA; text: kvp_cache_last_error(NULL). */
+/* k, v and the workspace are borrowed; the workspace's counters are zeroed here (the device is synchronised before that and
+   before return: not while a stream is captured).  Errors: INVALID, CAPACITY (workspace too small), CUDA; text: kvp_cache_last_error(NULL). */
 KVP_API int32_t kvp_cache_create(const kvp_cache_config *cfg, kvp_cache **out);
+
+/* Frees host resources, at once: launches that are under way, and recorded ones, go on using the memory that was lent. */
 KVP_API int32_t kvp_cache_destroy(kvp_cache *cache);
 
 /*

@@ -545,7 +545,8 @@ def norm_rope(q, k, positions, rope: Optional[Rope], q_out=None, k_out=None, q_w
 class PagedCache:
     """``kvp_cache`` over the caller's page tensors: ``k``, ``v`` = [layer][page][kv head][row][d] (order "heads") or
     [layer][page][row][kv head][d] ("tokens"), with any strides.  CPU tensors make a host-only cache: pages are counted,
-    nothing runs."""
+    nothing runs.  attend calls of one cache share its workspace: they have to be ordered among each other, recorded ones too,
+    and the cache has to outlive the graphs that hold them."""
 
     def __init__(self, k, v, n_q_heads: int, order: str = "heads", max_batch: int = 64, softmax_scale: float = 0.0):
         import torch
@@ -579,6 +580,11 @@ class PagedCache:
 
     def close(self):
         if self._h:
+            if self.workspace is not None:
+                # calls on other streams may still use it; while something is recorded nothing may be waited for
+                import torch
+                if not torch.cuda.is_current_stream_capturing():
+                    torch.cuda.synchronize(self.device)
             self._L.kvp_cache_destroy(self._h)
             self._h = ctypes.c_void_p()
 

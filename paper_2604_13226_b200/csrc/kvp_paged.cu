@@ -494,6 +494,9 @@ struct on_device {
 
 bool odd16(const void *p) { return ((uintptr_t)p & 15) != 0; }
 
+int32_t unit_shift_of(const kvp_cache_config *c);
+bool rows_fit(const kvp_cache_config *c);
+
 bool valid_cache(const kvp_cache_config *c)
 {
     if (!c || c->struct_bytes != (int32_t)sizeof(kvp_cache_config)) return false;
@@ -514,7 +517,21 @@ bool valid_cache(const kvp_cache_config *c)
     if ((c->n_layers > 1 && c->layer_stride < c->head_dim) || (c->n_pages > 1 && c->page_stride < c->head_dim) ||
         (c->n_kv_heads > 1 && c->head_stride < c->head_dim) || (c->page_size > 1 && c->row_stride < c->head_dim))
         return false;
-    return true;
+    return rows_fit(c);
+}
+
+// The largest power of two that divides all strides within a layer, in bytes; with it every row of a layer has to have a
+// number of 32 bits.
+int32_t unit_shift_of(const kvp_cache_config *c)
+{
+    const int64_t e = c->dtype == KVP_DTYPE_BF16 ? 2 : 4;
+    return __builtin_ctzll((uint64_t)((c->page_stride | c->head_stride | c->row_stride) * e) | (1ull << 40));
+}
+bool rows_fit(const kvp_cache_config *c)
+{
+    const double e = c->dtype == KVP_DTYPE_BF16 ? 2 : 4;
+    const double bytes = e * ((double)c->page_stride * (c->n_pages - 1) + (double)c->head_stride * (c->n_kv_heads - 1) + (double)c->row_stride * (c->page_size - 1));
+    return bytes / (double)(1ull << unit_shift_of(c)) < 4294967296.0;
 }
 
 struct cache_layout { uint64_t o, ml, arrived, total; int32_t units; };
@@ -722,6 +739,7 @@ int32_t kvp_cache_create(const kvp_cache_config *cfg, kvp_cache **out)
     c->elem_bytes = cfg->dtype == KVP_DTYPE_BF16 ? 2 : 4;
     c->scale = (float)(cfg->softmax_scale > 0.0 ? cfg->softmax_scale : 1.0 / sqrt((double)cfg->head_dim));
     c->by_page = divisor(cfg->page_size);
+    c->unit_shift = unit_shift_of(cfg);
     auto bail = [&](int32_t code) {
         delete c;
         return code;
@@ -759,10 +777,6 @@ int32_t kvp_cache_create(const kvp_cache_config *cfg, kvp_cache **out)
 int32_t kvp_cache_destroy(kvp_cache *c)
 {
     if (!c) return KVP_ERR_INVALID;
-    if (c->cfg.device >= 0) {
-        on_device dev(c->cfg.device);
-        if (dev.rc == cudaSuccess) (void)cudaDeviceSynchronize();
-    }
     delete c;
     return KVP_OK;
 }
@@ -806,6 +820,10 @@ int32_t kvp_cache_attend(kvp_cache *c, int32_t layer, int32_t batch, const void 
     if (batch == 0) return KVP_OK;
     kvp_paged_args a;
     a.st = store_of(c, layer);
+    a.unit_shift = c->unit_shift;
+    a.page_units = (uint32_t)(a.st.page_stride >> a.unit_shift);
+    a.head_units = (uint32_t)(a.st.head_stride >> a.unit_shift);
+    a.row_units = (uint32_t)(a.st.row_stride >> a.unit_shift);
     a.q = (const char *)q;
     a.out = (char *)out;
     for (int k = 0; k < 2; ++k) {

@@ -35,6 +35,8 @@ struct kvp_paged_ws {
 
 struct kvp_paged_args {
     kvp_store st;              // the layer's
+    uint32_t page_units, head_units, row_units;    // its strides in units of 2^unit_shift bytes, which divide all of them
+    int32_t unit_shift;
     const char *q;
     char *out;
     int64_t q_stride[2], out_stride[2];    // {request, head}, bytes
@@ -58,7 +60,7 @@ cudaError_t kvp_launch_paged_attn(const kvp_paged_args &a, int32_t dtype, int32_
 
 struct kvp_cache {
     kvp_cache_config cfg;
-    int32_t elem_bytes, sm_count = 148;
+    int32_t elem_bytes, sm_count = 148, unit_shift = 0;
     float scale;
     kvp_divisor by_page;
     kvp_paged_ws ws = {};

@@ -71,16 +71,17 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack(__nv_bfloat16 lo, __nv_bfloat16 hi)
+__device__ __forceinline__ uint32_t pack(float lo, float hi)
 {
-    return (uint32_t)__bfloat16_as_ushort(lo) | (uint32_t)__bfloat16_as_ushort(hi) << 16;
+    uint32_t x;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(hi), "f"(lo));
+    return x;
 }
 // a probability pair in two bf16 numbers each, value and rounding remainder
 __device__ __forceinline__ void split(float p0, float p1, uint32_t &value, uint32_t &rest)
 {
-    const __nv_bfloat16 h0 = __float2bfloat16_rn(p0), h1 = __float2bfloat16_rn(p1);
-    value = pack(h0, h1);
-    rest = pack(__float2bfloat16_rn(p0 - __bfloat162float(h0)), __float2bfloat16_rn(p1 - __bfloat162float(h1)));
+    value = pack(p0, p1);
+    rest = pack(p0 - __uint_as_float(value << 16), p1 - __uint_as_float(value & 0xffff0000u));
 }
 
 __device__ __forceinline__ float quad_max(float x)
@@ -275,19 +276,22 @@ template <typename T, int D, int W> struct loader {
         const place x = next[0];
         if (x.page != -2) {
             const int lane = threadIdx.x % 32;
-            const int64_t off = x.page < 0 ? 0 : x.page * a.st.page_stride + x.head * a.st.head_stride + x.row * a.st.row_stride;
+            // (in units that every row's place is a multiple of: 32 bits say it, whatever the size of the store)
+            const uint32_t off = x.page < 0 ? 0 : (uint32_t)x.page * a.page_units + (uint32_t)x.head * a.head_units + (uint32_t)x.row * a.row_units;
             const uint32_t there = __ballot_sync(0xffffffffu, x.page >= 0);
             if (lane == 0) *mask = there;
             constexpr int N = S::kKeys * S::kWords / 32;
+            const int c = lane % S::kWords;                // the same word of every row that this lane copies
+            const char *k = a.st.k + c * 16, *v = a.st.v + c * 16;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int y = i * 32 + lane, r = y / S::kWords, c = y % S::kWords;
-                const int64_t o = __shfl_sync(0xffffffffu, off, r) + c * 16;
+                const int r = (i * 32 + lane) / S::kWords;
+                const int64_t o = (int64_t)__shfl_sync(0xffffffffu, off, r) << a.unit_shift;
                 const bool in = (there >> r) & 1;
                 // bf16 rows are read by ldmatrix, eight rows at a time: the words of a row are permuted by its number
                 const uint32_t to = stage + r * S::kRowBytes + (sizeof(T) == 2 ? c ^ (r & 7) : c) * 16;
-                copy16(to, a.st.k + o, in);
-                copy16(to + S::kKeys * S::kRowBytes, a.st.v + o, in);
+                copy16(to, k + o, in);
+                copy16(to + S::kKeys * S::kRowBytes, v + o, in);
             }
         }
         copies_commit();
@@ -309,7 +313,7 @@ template <typename T> __host__ __device__ constexpr int unit_rows(bool wide) { r
 template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
     using S = shape<__nv_bfloat16, D>;
     static constexpr int kHalves = WIDE ? 2 : 1;           // rows of 8 that a thread has one of each
-    uint32_t q[D / 16][4];
+    uint32_t q[D / 16][2 * kHalves];
     float o[D / 8][4];
     float m[2], l[2];
 
@@ -319,11 +323,11 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < kHalves; ++h) {
                 const char *p = q0 + (g + 8 * h) * head_stride + (k * 16 + t * 2) * 2;
                 const bool in = g + 8 * h < n_rows;
                 q[k][h] = in ? *reinterpret_cast<const uint32_t *>(p) : 0u;
-                q[k][h + 2] = in ? *reinterpret_cast<const uint32_t *>(p + 16) : 0u;
+                q[k][h + kHalves] = in ? *reinterpret_cast<const uint32_t *>(p + 16) : 0u;
             }
         }
     }
@@ -335,13 +339,15 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
         l[0] = l[1] = 0.0f;
     }
 
-    __device__ void tile(uint32_t stage, uint32_t there, float scale)
+    __device__ void tile(uint32_t stage, uint32_t there, float scale, bool fresh)
     {
         const int lane = threadIdx.x % 32, t = lane % 4;
         constexpr int N = S::kKeys / 8;                    // 8-key columns of S
-        float s[N][4];
+        float s[N][4], s1[N][4];                           // even and odd steps of the dot products: two chains, half as long
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.0f;
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[i][e] = s1[i][e] = 0.0f;
         const int mi = lane / 8, mr = lane % 8;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
@@ -350,10 +356,15 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
             for (int k = 0; k < D / 16; ++k) {
                 uint32_t f[4];
                 ldmatrix4(stage + row * S::kRowBytes + (((k * 2 + (mi & 1)) ^ mr) * 16), f);
-                mma16816(s[2 * i], q[k], f[0], f[1]);
-                mma16816(s[2 * i + 1], q[k], f[2], f[3]);
+                const uint32_t qa[4] = {q[k][0], WIDE ? q[k][1] : 0u, q[k][kHalves], WIDE ? q[k][2 * kHalves - 1] : 0u};
+                mma16816(k % 2 ? s1[2 * i] : s[2 * i], qa, f[0], f[1]);
+                mma16816(k % 2 ? s1[2 * i + 1] : s[2 * i + 1], qa, f[2], f[3]);
             }
         }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 2 * kHalves; ++e) s[i][e] += s1[i][e];
         float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -378,7 +389,7 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
                 moved = true;
             }
         }
-        if (__any_sync(0xffffffffu, moved)) {
+        if (__any_sync(0xffffffffu, moved) && !fresh) {      // (a unit's first tile has nothing to scale)
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 o[i][0] *= fix[0];
@@ -476,7 +487,7 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
         l = 0.0f;
     }
 
-    __device__ void tile(uint32_t stage, uint32_t there, float scale)
+    __device__ void tile(uint32_t stage, uint32_t there, float scale, bool fresh)
     {
         const int lane = threadIdx.x % 32, part = lane % 8, key4 = lane / 8;
         constexpr int N = S::kKeys / 4;
@@ -518,7 +529,7 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
         const float fix = moved ? exp2_fast(m - top) : 1.0f, ref = top == -INFINITY ? 0.0f : top;
         m = top;
         l *= fix;
-        if (__any_sync(0xffffffffu, moved)) {
+        if (__any_sync(0xffffffffu, moved) && !fresh) {      // (a unit's first tile has nothing to scale)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float f = __shfl_sync(0xffffffffu, fix, r);
@@ -578,8 +589,8 @@ __device__ __forceinline__ void write_row(const kvp_paged_args &a, int b, int he
     char *to = a.out + b * a.out_stride[0] + head * a.out_stride[1] + c4 * 4 * sizeof(T);
     if (sizeof(T) == 2) {
         uint2 x;
-        x.x = pack(__float2bfloat16_rn(o.x), __float2bfloat16_rn(o.y));
-        x.y = pack(__float2bfloat16_rn(o.z), __float2bfloat16_rn(o.w));
+        x.x = pack(o.x, o.y);
+        x.y = pack(o.z, o.w);
         *reinterpret_cast<uint2 *>(to) = x;
     } else {
         *reinterpret_cast<float4 *>(to) = o;
@@ -732,6 +743,7 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
         if (!more) break;
         p = p1;
         tm.begin();
+        bool fresh = true;
 #pragma unroll 1
         for (int t = p.lo + (warp + W - turn) % W; t < p.hi; t += W) {
             copies_wait<kStages - 2>();
@@ -740,7 +752,8 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
             const uint32_t there = masks[warp][stage];
             ld.issue(a, ring + ahead * kStageBytes, &masks[warp][ahead]);
             ld.look_up(a, ln, units, row_tiles);
-            tm.tile(ring + stage * kStageBytes, there, scale);
+            tm.tile(ring + stage * kStageBytes, there, scale, fresh);
+            fresh = false;
             stage = stage == kStages - 1 ? 0 : stage + 1;
         }
         turn = (turn + p.hi - p.lo) % W;
