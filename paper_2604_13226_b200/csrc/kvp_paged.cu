@@ -581,6 +581,8 @@ int32_t token_args(kvp_cache *c, const kvp_tokens *t, const kvp_rope *rope, int3
 {
     if (!t || t->struct_bytes != (int32_t)sizeof(kvp_tokens)) return fail(c, KVP_ERR_INVALID, "tokens: not a kvp_tokens of this version");
     if (t->n_tokens < 0) return fail(c, KVP_ERR_INVALID, "tokens: n_tokens is negative");
+    a.n_tokens = 0;
+    if (t->n_tokens == 0) return KVP_OK;           // nothing to do, and arrays of nothing have no address
     if ((t->q != nullptr) != (t->q_out != nullptr)) return fail(c, KVP_ERR_INVALID, "tokens: q and q_out go together");
     if (t->n_q_heads < 0 || t->n_q_heads > 65535 || t->n_kv_heads < 0 || t->n_kv_heads > 65535 || (t->q && t->n_q_heads == 0) || (t->k && t->n_kv_heads == 0))
         return fail(c, KVP_ERR_INVALID, "tokens: number of heads");
