@@ -79,6 +79,7 @@ struct append_args {
     kvp_store st;                  // st.k null: no pages
     int32_t n_tokens, n_q, n_k, n_v;   // heads of each that there is something to do for
     int32_t rotary, pairing;
+    int32_t half_q, half_kv;       // q heads of a half of a token, and its k and v heads
     float eps, magnitude;
     double turns[64];              // f_i / 2 pi
 };
@@ -169,10 +170,8 @@ __device__ __forceinline__ uint4 *words_at(const rows_at &r, int token, int head
 // A token's row in the pages.
 struct page_row {
     char *k, *v;                   // null: nowhere
-    __device__ page_row(const append_args &a, int token) : k(nullptr), v(nullptr)
+    __device__ page_row(const append_args &a, int32_t slot) : k(nullptr), v(nullptr)
     {
-        if (!a.st.k) return;
-        const int32_t slot = a.slots[token];
         if (slot < 0 || slot >= a.st.n_pages * a.st.page_size) return;
         const int32_t page = divide(slot, a.st.by_page), row = slot - page * a.st.page_size;
         const int64_t at = page * a.st.page_stride + row * a.st.row_stride;
@@ -204,9 +203,11 @@ __device__ __forceinline__ float2 angle_of(int position, double turns, float mag
     return make_float2(magnitude * cosine, magnitude * sine);
 }
 
-// Many tokens: bound by DRAM.  A thread has four rows under way; blocks take tokens in turn, so that the frequencies are fetched
-// once (a token per warp and launch: 33,280 tokens 141 us, in turn 133; in one wave 131, but 8,000 tokens 73 instead of 64).
-template <typename T, int D>
+// Many tokens: bound by DRAM (33,280 tokens of 32/8 heads of 128 with norms: 130 us, 6.3 TB/s read and written; a copy reaches
+// 6.5).  A thread has four rows under way; warps take tokens in turn, so that the frequencies are fetched once (a token per
+// warp and launch: 141 us), and the next token's position and slot are fetched a token ahead (137 without).  HALVES: a warp
+// has half of one token's heads - where warps are left over (1,000 tokens: 8.9 us whole, 6.1 in halves; 2,048: 10.9, 14.7).
+template <typename T, int D, bool HALVES>
 __global__ void __launch_bounds__(256, 2)
 append_many_kernel(const __grid_constant__ append_args a)
 {
@@ -220,7 +221,13 @@ append_many_kernel(const __grid_constant__ append_args a)
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) f[i] = lane + 32 * i < a.rotary / 2 ? a.turns[lane + 32 * i] : 0.0;
     pdl_wait();
-    for (int token = blockIdx.x * 8 + warp; token < a.n_tokens; token += gridDim.x * 8) {
+    const int first = blockIdx.x * 8 + warp, part = HALVES ? first & 1 : 0;
+    int token = HALVES ? first / 2 : first;
+    if (token >= a.n_tokens) return;
+    int position = a.rotary ? a.positions[token] : 0, slot = a.st.k ? a.slots[token] : -1;
+    while (true) {
+        const int next = token + gridDim.x * 8, next_position = next < a.n_tokens && a.rotary ? a.positions[next] : 0;
+        const int next_slot = next < a.n_tokens && a.st.k ? a.slots[next] : -1;
         uint4 x[U], y[U];
         auto fetch = [&](const rows_at &r, int u, int head, int end) {
             if (head >= end) return;
@@ -232,10 +239,10 @@ append_many_kernel(const __grid_constant__ append_args a)
             p[m.w0] = x[u];
             p[m.w1] = y[u];
         };
-        const int position = a.rotary ? a.positions[token] : 0;
-        const page_row to(a, token);
+        const int q0 = HALVES ? part * a.half_q : 0, q1 = HALVES ? min(q0 + a.half_q, a.n_q) : a.n_q;
+        const int kv0 = HALVES ? part * a.half_kv : 0, k1 = HALVES ? min(kv0 + a.half_kv, a.n_k) : a.n_k, v1 = HALVES ? min(kv0 + a.half_kv, a.n_v) : a.n_v;
 #pragma unroll
-        for (int u = 0; u < U; ++u) fetch(a.q, u, mine + u * R, a.n_q);
+        for (int u = 0; u < U; ++u) fetch(a.q, u, q0 + u * R + mine, q1);
         if (a.rotary) {
             __syncwarp();
 #pragma unroll
@@ -244,33 +251,38 @@ append_many_kernel(const __grid_constant__ append_args a)
             take_angles<T, D>(m, turned_by[warp], a.pairing);
         }
         if (a.q_weight) m.weigh(a.q_weight);
-        for (int h0 = 0; h0 < a.n_q; h0 += U * R) {
+        for (int h0 = q0; h0 < q1; h0 += U * R) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int head = h0 + u * R + mine;
-                if (head - mine >= a.n_q) break;
+                if (head - mine >= q1) break;
                 m.row(x[u], y[u], a.q_weight, a.q_weight, true, a.eps, a.pairing);
-                if (head < a.n_q) store(words_at(a.q_out, token, head), u);
+                if (head < q1) store(words_at(a.q_out, token, head), u);
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) fetch(a.q, u, h0 + (U + u) * R + mine, a.n_q);
+            for (int u = 0; u < U; ++u) fetch(a.q, u, h0 + (U + u) * R + mine, q1);
         }
         if (a.k_weight) m.weigh(a.k_weight);
-        for (int h0 = 0; h0 < max(a.n_k, a.n_v); h0 += U / 2 * R) {
+        const page_row to(a, slot);
+        for (int h0 = kv0; h0 < max(k1, v1); h0 += U / 2 * R) {
 #pragma unroll
             for (int u = 0; u < U / 2; ++u) {
-                fetch(a.k, u, h0 + u * R + mine, a.n_k);
-                fetch(a.v, U / 2 + u, h0 + u * R + mine, a.n_v);
+                fetch(a.k, u, h0 + u * R + mine, k1);
+                fetch(a.v, U / 2 + u, h0 + u * R + mine, v1);
             }
 #pragma unroll
             for (int u = 0; u < U / 2; ++u) {
                 const int head = h0 + u * R + mine;
-                if (head - mine < a.n_k) m.row(x[u], y[u], a.k_weight, a.k_weight, true, a.eps, a.pairing);
-                if (head < a.n_k && a.k_out.p) store(words_at(a.k_out, token, head), u);
-                if (head < a.n_k && to.k) store(reinterpret_cast<uint4 *>(to.k + head * a.st.head_stride), u);
-                if (head < a.n_v && to.v) store(reinterpret_cast<uint4 *>(to.v + head * a.st.head_stride), U / 2 + u);
+                if (head - mine < k1) m.row(x[u], y[u], a.k_weight, a.k_weight, true, a.eps, a.pairing);
+                if (head < k1 && a.k_out.p) store(words_at(a.k_out, token, head), u);
+                if (head < k1 && to.k) store(reinterpret_cast<uint4 *>(to.k + head * a.st.head_stride), u);
+                if (head < v1 && to.v) store(reinterpret_cast<uint4 *>(to.v + head * a.st.head_stride), U / 2 + u);
             }
         }
+        if (HALVES || next >= a.n_tokens) return;
+        token = next;
+        position = next_position;
+        slot = next_slot;
     }
 }
 
@@ -314,7 +326,7 @@ append_few_kernel(const __grid_constant__ append_args a)
     if (kind == 0) store(words_at(a.q_out, token, head));
     if (kind == 1 && a.k_out.p) store(words_at(a.k_out, token, head));
     if (kind == 1 || kind == 2) {
-        const page_row to(a, token);
+        const page_row to(a, a.st.k ? a.slots[token] : -1);
         if (to.k) store(reinterpret_cast<uint4 *>((kind == 1 ? to.k : to.v) + head * a.st.head_stride));
     }
 }
@@ -329,10 +341,17 @@ kvp_divisor divisor(int32_t d)
 template <typename T, int D>
 cudaError_t launch_append(append_args &a, int sm_count, cudaStream_t st)
 {
-    // 512 tokens of 32/8 heads: 7.1 us as many, 5.9 as few; 1,000 of 28/4: 8.8, 11.4.  Twice as many blocks as fit, so that the
-    // last ones even out.
-    if (a.n_tokens >= 4 * sm_count)
-        return launch_pdl(append_many_kernel<T, D>, dim3(std::min((a.n_tokens + 7) / 8, 4 * sm_count)), dim3(256), 0, st, a);
+    // 512 tokens of 32/8 heads: 7.1 us as many, 4.9 as few; 1,000 of 28/4: 6.1, 11.4.  Twice as many blocks as fit, so that the last
+    // ones even out (one wave: 8,000 tokens of fp32 73 us instead of 65).
+    if (a.n_tokens >= 4 * sm_count) {
+        if (a.n_tokens <= 8 * sm_count) {
+            const int at_once = row_math<T, D>::R, kv = std::max(a.n_k, a.n_v);
+            a.half_q = (a.n_q + 2 * at_once - 1) / (2 * at_once) * at_once;
+            a.half_kv = (kv + 2 * at_once - 1) / (2 * at_once) * at_once;
+            return launch_pdl(append_many_kernel<T, D, true>, dim3((2 * a.n_tokens + 7) / 8), dim3(256), 0, st, a);
+        }
+        return launch_pdl(append_many_kernel<T, D, false>, dim3(std::min((a.n_tokens + 7) / 8, 4 * sm_count)), dim3(256), 0, st, a);
+    }
     const int rows = a.n_q + a.n_k + a.n_v, at_once = 256 / row_math<T, D>::L;
     return launch_pdl(append_few_kernel<T, D>, dim3(a.n_tokens, (rows + at_once - 1) / at_once), dim3(256), 0, st, a);
 }
