@@ -238,3 +238,29 @@ def test_a_cache_that_goes_while_something_is_recorded():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.float32, 64), (torch.bfloat16, 128), (torch.bfloat16, 64)])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (7, 1), (12, 3), (33, 11), (0, 2)])
+@pytest.mark.parametrize("n", [591, 592, 700, 1184, 1185, 5000])
+def test_appends_of_every_length(dtype, d, hq, hkv, n):
+    """Few tokens, a few thousand, many: each has its own way to share heads out, odd numbers of heads among them."""
+    page, n_pages = 16, -(-n // 16) + 1
+    k, v = ref.pages((1, n_pages, hkv, page, d), "heads", dtype, seed=n)
+    c = kvp.PagedCache(k, v, max(1, hq) * hkv if hq % hkv else max(hq, hkv))
+    qkv = torch.randn(n, max(1, c.n_q_heads) + 2 * hkv, d, device="cuda").to(dtype)
+    nq = c.n_q_heads if hq else 0
+    q, kn, vn = (qkv[:, :nq], qkv[:, nq:nq + hkv], qkv[:, nq + hkv:nq + 2 * hkv])
+    g = torch.Generator().manual_seed(n)
+    slots = torch.randperm(n_pages * page, generator=g)[:n].int().cuda()
+    pos = torch.randint(0, 1 << 17, (n,), generator=g).int().cuda()
+    w = (1 + 0.2 * torch.randn(d, device="cuda")).to(dtype)
+    q_out = torch.empty(n, nq, d, device="cuda", dtype=dtype) if nq else None
+    c.append(0, kn, vn, pos, slots, rope=kvp.Rope(d, rotary_dim=48, theta=1e6), q=q if nq else None, q_out=q_out, q_weight=w if nq else None, k_weight=w)
+    f = ref.frequencies(48, 1e6)
+    s = slots.long()
+    got = [(k[0, s // page, :, s % page], kn)] + ([(q_out, q)] if nq else [])
+    for x, src in got:
+        want, tol = ref.norm_rotate(src, w, 1e-6, pos, f, 0, 1.0)
+        ref.check(x, want, tol + 1.001 * ref.HALF_STEP[dtype] * want.abs())
+    assert torch.equal(v[0, s // page, :, s % page], vn)
