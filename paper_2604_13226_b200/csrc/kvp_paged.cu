@@ -13,28 +13,6 @@
 
 namespace {
 
-// Two fp32 numbers in a register pair, and the packed arithmetic on them.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float lo, float hi)
-{
-    f32x2 x;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
-    return x;
-}
-__device__ __forceinline__ void unpack2(f32x2 x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
-{
-    f32x2 x;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
-{
-    f32x2 x;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
-    return x;
-}
-
 // A 16-byte word of elements as pairs of fp32 numbers, and back (rounded to nearest).
 template <typename T> struct elem;
 template <> struct elem<float> {

@@ -24,6 +24,28 @@ struct kvp_store {
 
 #ifdef __CUDACC__
 __device__ __forceinline__ int32_t divide(int32_t n, kvp_divisor d) { return (int32_t)(((uint64_t)(uint32_t)n * d.mul) >> d.shift); }
+
+// Two fp32 numbers in a register pair, and the packed arithmetic on them.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi)
+{
+    f32x2 x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(lo), "f"(hi));
+    return x;
+}
+__device__ __forceinline__ void unpack2(f32x2 x, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
 #endif
 
 // Partial results of units whose rows several CTAs share, and a count of the parts that are in per unit.

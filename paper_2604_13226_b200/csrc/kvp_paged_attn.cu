@@ -456,13 +456,15 @@ template <int D, bool WIDE> struct tile_math<__nv_bfloat16, D, WIDE> {
     }
 };
 
-// fp32: FMA pipe.  Q K^T: 8 lanes share a key, each with a sixteenth or an eighth of its words, four keys at once; P V: a lane
-// has D/32 columns of every row.  4 query rows, or 8 (WIDE).
+// fp32: FMA pipe, two numbers an instruction.  Q K^T: 8 lanes share a key, each with an eighth of its words, four keys at once;
+// P V: a lane has D/32 columns of every row.  4 query rows, or 8 (WIDE).  Twice as many instructions, and probabilities handed
+// round by shuffles, took 8 x 8,000 rows of 28/4 heads from 50.8 us to 54.0, heads of 64 from 31.6 to 35.7 (4 rows: no difference,
+// DRAM).
 template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
     using S = shape<float, D>;
     static constexpr int R = WIDE ? 8 : 4, C = D / 32;
-    float q[R][D / 8];
-    float o[R][C];
+    f32x2 q[R][D / 16];
+    f32x2 o[R / 2][C];                     // rows 2i and 2i + 1
     float m, l;                            // of row (lane % R)
 
     __device__ void queries(const char *q0, int64_t head_stride, int n_rows)
@@ -474,15 +476,16 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
             for (int j = 0; j < D / 32; ++j) {
                 float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (r < n_rows) x = *reinterpret_cast<const float4 *>(q0 + r * head_stride + (j * 8 + part) * 16);
-                q[r][4 * j] = x.x; q[r][4 * j + 1] = x.y; q[r][4 * j + 2] = x.z; q[r][4 * j + 3] = x.w;
+                q[r][2 * j] = pack2(x.x, x.y);
+                q[r][2 * j + 1] = pack2(x.z, x.w);
             }
     }
     __device__ void begin()
     {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R / 2; ++r)
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[r][c] = 0.0f;
+            for (int c = 0; c < C; ++c) o[r][c] = 0;
         m = -INFINITY;
         l = 0.0f;
     }
@@ -494,16 +497,22 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
         float s[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float x[R];
+            f32x2 x2[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) x[r] = 0.0f;
+            for (int r = 0; r < R; ++r) x2[r] = 0;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
-                float4 k;
-                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(k.x), "=f"(k.y), "=f"(k.z), "=f"(k.w)
-                             : "r"(stage + (i * 4 + key4) * S::kRowBytes + (j * 8 + part) * 16) : "memory");
+                f32x2 k0, k1;
+                asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(k0), "=l"(k1) : "r"(stage + (i * 4 + key4) * S::kRowBytes + (j * 8 + part) * 16) : "memory");
 #pragma unroll
-                for (int r = 0; r < R; ++r) x[r] += q[r][4 * j] * k.x + q[r][4 * j + 1] * k.y + q[r][4 * j + 2] * k.z + q[r][4 * j + 3] * k.w;
+                for (int r = 0; r < R; ++r) x2[r] = fma2(q[r][2 * j + 1], k1, fma2(q[r][2 * j], k0, x2[r]));
+            }
+            float x[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float lo, hi;
+                unpack2(x2[r], lo, hi);
+                x[r] = lo + hi;
             }
             // the 8 lanes of a key add up; lane `part` keeps row `part % R`
             if (R == 4) {
@@ -531,31 +540,37 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
         l *= fix;
         if (__any_sync(0xffffffffu, moved) && !fresh) {      // (a unit's first tile has nothing to scale)
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const float f = __shfl_sync(0xffffffffu, fix, r);
+            for (int r = 0; r < R; r += 2) {
+                const f32x2 f = pack2(__shfl_sync(0xffffffffu, fix, r), __shfl_sync(0xffffffffu, fix, r + 1));
 #pragma unroll
-                for (int c = 0; c < C; ++c) o[r][c] *= f;
+                for (int c = 0; c < C; ++c) o[r / 2][c] = mul2(o[r / 2][c], f);
             }
         }
-        const uint32_t v = stage + S::kKeys * S::kRowBytes;
+        // the probabilities go round the warp through the keys' place, which has been read: [key][row]
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float p = exp2_fast(s[i] - ref);
             l += p;                                        // of the keys of this lane
+            if (part < R) asm volatile("st.shared.f32 [%0], %1;" ::"r"(stage + ((i * 4 + key4) * R + part) * 4), "f"(p) : "memory");
+        }
+        __syncwarp();
+        const uint32_t v = stage + S::kKeys * S::kRowBytes;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float x[C];
-                if (C == 4)
-                    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[C - 2]), "=f"(x[C - 1])
-                                 : "r"(v + (i * 4 + k) * S::kRowBytes + lane * 16) : "memory");
-                else
-                    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(v + (i * 4 + k) * S::kRowBytes + lane * 8) : "memory");
+        for (int i = 0; i < S::kKeys; ++i) {
+            f32x2 w[R / 2];
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const float w = __shfl_sync(0xffffffffu, p, k * 8 + r);
+            for (int r = 0; r < R / 2; r += 2) asm volatile("ld.shared.v2.b64 {%0,%1}, [%2];" : "=l"(w[r]), "=l"(w[r + 1]) : "r"(stage + (i * R + 2 * r) * 4) : "memory");
+            float x[C];
+            if (C == 4)
+                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[C - 2]), "=f"(x[C - 1]) : "r"(v + i * S::kRowBytes + lane * 16) : "memory");
+            else
+                asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(v + i * S::kRowBytes + lane * 8) : "memory");
 #pragma unroll
-                    for (int c = 0; c < C; ++c) o[r][c] += w * x[c];
-                }
+            for (int c = 0; c < C; ++c) {
+                const f32x2 x2 = pack2(x[c], x[c]);
+#pragma unroll
+                for (int r = 0; r < R / 2; ++r) o[r][c] = fma2(w[r], x2, o[r][c]);
             }
         }
     }
@@ -571,9 +586,15 @@ template <int D, bool WIDE> struct tile_math<float, D, WIDE> {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (r >= n) break;
+            float x[C], other;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (r % 2) unpack2(o[r / 2][c], other, x[c]);
+                else unpack2(o[r / 2][c], x[c], other);
+            }
             float *to = out + join_at<D>(r, lane * C);
-            if (C == 4) *reinterpret_cast<float4 *>(to) = make_float4(o[r][0], o[r][1], o[r][C - 2], o[r][C - 1]);
-            else *reinterpret_cast<float2 *>(to) = make_float2(o[r][0], o[r][1]);
+            if (C == 4) *reinterpret_cast<float4 *>(to) = make_float4(x[0], x[1], x[C - 2], x[C - 1]);
+            else *reinterpret_cast<float2 *>(to) = make_float2(x[0], x[1]);
         }
         if (lane < n) ml[lane] = make_float2(m, l);
     }
