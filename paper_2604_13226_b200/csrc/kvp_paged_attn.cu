@@ -2,8 +2,10 @@
 //
 // out = sum_j softmax(scale q.k_j) v_j over the request's visible rows, the group's query heads together against their kv head.
 // Every K and V byte is used for at most 16 query rows, so reading the cache bounds the call: 6.5 TB/s are 23 bytes per SM and
-// clock, 350 clocks for the 8 KB of 16 keys of 128 in bf16, where mma.sync needs 64 of them.  What matters is bytes in flight
-// and an even share for every SM.
+// clock, 350 clocks for the 8 KB of 16 keys of 128 in bf16, where mma.sync needs 64 of them (the tensor pipe is 21 % busy);
+// tiles of 128 rows, as tcgen05 has them, would be empty but for a few.  16 requests of 33,280 rows, 32/8 heads, take 325 us =
+// 6.7 TB/s, one of 133,120 rows 88 us = 6.2 TB/s (DRAM is read at 7.5 TB/s while tiles stream; 3 us go by before the first
+// rows are asked for, CTAs end 3 us before and after their mean, arriving and joining takes 3), one of 2,785 rows 8.5 us.
 //
 // * A unit is (request, kv head, up to 16 of its query heads).  Units are laid end to end, a unit counting as long as its key
 //   tiles plus a fixed cost, and the line is cut into equal shares, one per CTA.  Every CTA finds its share itself, from the
