@@ -449,7 +449,7 @@ KVP_API int32_t kvp_rope_frequencies(const kvp_rope *rope, double *inv_freq);
  */
 typedef struct kvp_tokens {
     int32_t struct_bytes;       /* = sizeof(kvp_tokens)                                               */
-    int32_t n_tokens;           /* >= 0                                                               */
+    int32_t n_tokens;           /* 0 to 2^30                                                          */
     int32_t n_q_heads, n_kv_heads;
     const void *q, *k, *v;      /* device; q or k may be NULL (its output too); v only for kvp_cache_append */
     void *q_out, *k_out;        /* device; may be q and k themselves (with the same strides)          */
@@ -523,7 +523,7 @@ KVP_API int32_t kvp_cache_append(kvp_cache *cache, int32_t layer, const kvp_toke
  * appended): softmax in fp32, q head h reads kv head h / (Hq/Hkv).
  *   q      device, {batch, head} strides in elements; out likewise.  16-byte aligned, strides multiples of 16 bytes
  *   table  device [batch][table_cols] with row stride table_stride: page numbers; n_kv_heads * batch * (table_cols *
- *          page_size / 8 + 9), for groups of more than 8 heads once for each 8, is below 2^31
+ *          page_size / 8 + 17), for groups of more than 8 heads once for each 8, is below 2^31
  *   lens, first   device [batch]; first may be NULL (0).  Lengths beyond table_cols pages end there.  A request without a
  *          row gets zeros and an lse of minus infinity
  *   lse    device float [batch][n_q_heads] or NULL

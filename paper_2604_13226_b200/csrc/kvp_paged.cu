@@ -492,6 +492,21 @@ struct on_device {
 
 bool odd16(const void *p) { return ((uintptr_t)p & 15) != 0; }
 
+// Whether rows of `width` elements, numbered by n indices of the given counts and strides, lie apart: from the smallest stride on, each
+// step is as long as all that the ones before it reach.
+struct index_of_rows { int64_t count, stride; };
+bool rows_apart(index_of_rows *x, int n, int64_t width)
+{
+    std::sort(x, x + n, [](const index_of_rows &a, const index_of_rows &b) { return llabs(a.stride) < llabs(b.stride); });
+    double span = (double)width;
+    for (int i = 0; i < n; ++i) {
+        if (x[i].count <= 1) continue;
+        if ((double)llabs(x[i].stride) < span) return false;
+        span += (double)llabs(x[i].stride) * (double)(x[i].count - 1);
+    }
+    return true;
+}
+
 int32_t unit_shift_of(const kvp_cache_config *c);
 bool rows_fit(const kvp_cache_config *c);
 
@@ -511,11 +526,8 @@ bool valid_cache(const kvp_cache_config *c)
     const int64_t strides[4] = {c->layer_stride, c->page_stride, c->head_stride, c->row_stride};
     for (int64_t s : strides)
         if (s < 0 || s % unit || s > (1ll << 56)) return false;
-    // each index of more than one value moves by a row at least
-    if ((c->n_layers > 1 && c->layer_stride < c->head_dim) || (c->n_pages > 1 && c->page_stride < c->head_dim) ||
-        (c->n_kv_heads > 1 && c->head_stride < c->head_dim) || (c->page_size > 1 && c->row_stride < c->head_dim))
-        return false;
-    return rows_fit(c);
+    index_of_rows rows[4] = {{c->n_layers, c->layer_stride}, {c->n_pages, c->page_stride}, {c->n_kv_heads, c->head_stride}, {c->page_size, c->row_stride}};
+    return rows_apart(rows, 4, c->head_dim) && rows_fit(c);
 }
 
 // The largest power of two that divides all strides within a layer, in bytes; with it every row of a layer has to have a
@@ -578,7 +590,7 @@ double frequency(const kvp_rope *r, int i)
 int32_t token_args(kvp_cache *c, const kvp_tokens *t, const kvp_rope *rope, int32_t dtype, int32_t head_dim, append_args &a)
 {
     if (!t || t->struct_bytes != (int32_t)sizeof(kvp_tokens)) return fail(c, KVP_ERR_INVALID, "tokens: not a kvp_tokens of this version");
-    if (t->n_tokens < 0) return fail(c, KVP_ERR_INVALID, "tokens: n_tokens is negative");
+    if (t->n_tokens < 0 || t->n_tokens > (1 << 30)) return fail(c, KVP_ERR_INVALID, "tokens: n_tokens is negative or above 2^30");
     a.n_tokens = 0;
     if (t->n_tokens == 0) return KVP_OK;           // nothing to do, and arrays of nothing have no address
     if ((t->q != nullptr) != (t->q_out != nullptr)) return fail(c, KVP_ERR_INVALID, "tokens: q and q_out go together");
@@ -612,8 +624,8 @@ int32_t token_args(kvp_cache *c, const kvp_tokens *t, const kvp_rope *rope, int3
             x[i].to.stride[k] = x[i].s[k] * e;
         }
         // rows that are written must not lie over one another
-        if (i >= 3 && ((t->n_tokens > 1 && llabs(x[i].s[0]) < head_dim) || (x[i].heads > 1 && llabs(x[i].s[1]) < head_dim)))
-            return fail(c, KVP_ERR_INVALID, "tokens: rows of an output overlap");
+        index_of_rows rows[2] = {{t->n_tokens, x[i].s[0]}, {x[i].heads, x[i].s[1]}};
+        if (i >= 3 && !rows_apart(rows, 2, head_dim)) return fail(c, KVP_ERR_INVALID, "tokens: rows of an output overlap");
     }
     // in place only row for row
     if ((t->q && t->q_out == t->q && (t->q_stride[0] != t->q_out_stride[0] || t->q_stride[1] != t->q_out_stride[1])) ||
@@ -810,8 +822,8 @@ int32_t kvp_cache_attend(kvp_cache *c, int32_t layer, int32_t batch, const void 
         for (int k = 0; k < 2; ++k)
             if (llabs(q_stride[k]) > (1ll << 56) || llabs(out_stride[k]) > (1ll << 56) || q_stride[k] * c->elem_bytes % 16 || out_stride[k] * c->elem_bytes % 16)
                 return fail(c, KVP_ERR_INVALID, "attend: strides must be multiples of 16 bytes");
-        if ((batch > 1 && llabs(out_stride[0]) < c->cfg.head_dim) || (c->cfg.n_q_heads > 1 && llabs(out_stride[1]) < c->cfg.head_dim))
-            return fail(c, KVP_ERR_INVALID, "attend: rows of out overlap");
+        index_of_rows rows[2] = {{batch, out_stride[0]}, {c->cfg.n_q_heads, out_stride[1]}};
+        if (!rows_apart(rows, 2, c->cfg.head_dim)) return fail(c, KVP_ERR_INVALID, "attend: rows of out overlap");
         if (llabs(table_stride) > (1ll << 56)) return fail(c, KVP_ERR_INVALID, "attend: table_stride");
     }
     if (!kvp_paged_fits(batch, c->cfg.n_kv_heads, c->cfg.n_q_heads / c->cfg.n_kv_heads, std::min<int64_t>(INT32_MAX, (int64_t)table_cols * c->cfg.page_size)))

@@ -34,6 +34,8 @@ def refused(code, call, *a, **kw):
     lambda: kvp.PagedCache(*[torch.zeros(1, 1, 1, 4, 64).expand(1, 9, 2, 4, 64) for _ in range(2)], 4),       # pages on top of one another
     lambda: kvp.PagedCache(*[torch.zeros(2, 3, 2, 4, 66)[..., :64] for _ in range(2)], 4),                     # rows of 264 bytes
     lambda: kvp.PagedCache(*[torch.zeros(2, 3, 2, 4, 128)[..., ::2] for _ in range(2)], 4),
+    lambda: kvp.PagedCache(*[torch.zeros(4000).as_strided((2, 3, 2, 4, 64), (1024, 256, 128, 64, 1)) for _ in range(2)], 4),    # heads over one another
+    lambda: kvp.PagedCache(*[torch.zeros(4000).as_strided((2, 3, 2, 4, 64), (512, 512, 256, 64, 1)) for _ in range(2)], 4),     # layers over pages
 ])
 def test_configurations_that_are_refused(make):
     refused(INVALID, make)
@@ -171,6 +173,7 @@ def test_append_arguments():
            dict(slots=torch.zeros(3, dtype=torch.int64)), dict(slots=i(2)), dict(positions=i(4)), dict(positions=None), dict(k=t(3, 2, 128)[..., ::2]),
            dict(k=t(3, 2, 65)[..., 1:]), dict(k=t(3, 2, 66)[..., :64]), dict(k_weight=t(32)), dict(q_weight=t(64)), dict(k_weight=t(64), eps=-1.0),
            dict(k_weight=t(64), eps=math.nan), dict(q=q, q_out=t(3, 4, 64)[:1].expand(3, 4, 64)), dict(k_out=t(3, 1, 64).expand(3, 2, 64)),
+           dict(k_out=t(4, 64).as_strided((3, 2, 64), (64, 64, 1))), dict(k_out=t(8, 64).as_strided((3, 2, 64), (128, 192, 1))),
            dict(q=q, q_out=q.as_strided((3, 4, 64), (64, 192, 1))), dict(slots=i(6)[::2])]
     for kw in bad:
         a = dict(k=k, v=t(3, 2, 64), positions=i(3), slots=i(3), rope=kvp.Rope(64))
@@ -256,9 +259,16 @@ def test_attend_arguments():
     for kw in (dict(q=t(2, 2, 64)), dict(q=t(2, 4, 32)), dict(q=t(2, 4, 64).bfloat16()), dict(out=t(1, 4, 64)), dict(out=t(2, 4, 64).double()),
                dict(table=i(3, 3)), dict(table=i(2, 3).long()), dict(table=i(2, 6)[:, ::2]), dict(lens=i(3)), dict(lens=t(2)), dict(first=i(1)),
                dict(lse=t(2, 3)), dict(lse=t(4, 2).T), dict(lse=t(2, 4).double()), dict(q=t(2, 4, 65)[..., 1:]), dict(q=t(2, 4, 66)[..., :64]),
-               dict(out=t(1, 4, 64).expand(2, 4, 64)), dict(out=t(2, 1, 64).expand(2, 4, 64)), dict(lens=i(4)[::2])):
+               dict(out=t(1, 4, 64).expand(2, 4, 64)), dict(out=t(2, 1, 64).expand(2, 4, 64)), dict(lens=i(4)[::2]),
+               dict(out=t(6, 64).as_strided((2, 4, 64), (128, 64, 1)))):
         refused(INVALID, c.attend, 0, **dict(good, **kw))
     refused(STATE, c.attend, 0, **good)
+    refused(STATE, c.attend, 0, **dict(good, out=t(8, 64).as_strided((2, 4, 64), (64, 128, 1))))          # heads outermost: rows lie apart
+    # tables that could hold more tiles than are counted; nothing reads the addresses
+    c = cache(heads=8, hq=8, max_batch=3)
+    strides = (ctypes.c_int64 * 2)(512, 64)
+    call = lambda cols: kvp.lib().kvp_cache_attend(c._h, 0, 3, 1 << 20, strides, 1 << 20, cols, cols, 1 << 20, None, 1 << 20, strides, None, None)
+    assert call(2 ** 29) == CAPACITY and call(2 ** 20) == STATE
     refused(CAPACITY, c.attend, 0, t(4, 4, 64), i(4, 3), i(4), t(4, 4, 64))
 
 
