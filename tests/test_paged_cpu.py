@@ -265,9 +265,9 @@ def test_attend_arguments():
     refused(STATE, c.attend, 0, **good)
     refused(STATE, c.attend, 0, **dict(good, out=t(8, 64).as_strided((2, 4, 64), (64, 128, 1))))          # heads outermost: rows lie apart
     # tables that could hold more tiles than are counted; nothing reads the addresses
-    c = cache(heads=8, hq=8, max_batch=3)
+    wide = cache(heads=8, hq=8, max_batch=3)
     strides = (ctypes.c_int64 * 2)(512, 64)
-    call = lambda cols: kvp.lib().kvp_cache_attend(c._h, 0, 3, 1 << 20, strides, 1 << 20, cols, cols, 1 << 20, None, 1 << 20, strides, None, None)
+    call = lambda cols: kvp.lib().kvp_cache_attend(wide._h, 0, 3, 1 << 20, strides, 1 << 20, cols, cols, 1 << 20, None, 1 << 20, strides, None, None)
     assert call(2 ** 29) == CAPACITY and call(2 ** 20) == STATE
     refused(CAPACITY, c.attend, 0, t(4, 4, 64), i(4, 3), i(4), t(4, 4, 64))
 
