@@ -1,5 +1,6 @@
 """ctypes binding of ``libkvp.so`` - argument marshalling only; every step of the path runs in the
-library's CUDA kernels.  Function names mirror ``include/kvp.h``.
+library's CUDA kernels.  Function names mirror ``include/kvp.h``.  The paged cache's calls on tensors are marshalled by a
+module in C++ (``csrc/kvp_calls.cpp``); what it does not take is looked at here, and refused with the reason.
 
 PyTorch is used here for device memory and streams only (``Context`` accepts torch tensors and
 passes their ``data_ptr()``).  There is no CPU fallback: if the shared library is missing or cannot
@@ -8,6 +9,7 @@ be loaded, importing a symbol raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import struct
 from typing import List, Optional, Sequence, Tuple
@@ -151,6 +153,25 @@ EXPORTED = ["kvp_version", "kvp_token_bytes", "kvp_workspace_bytes", "kvp_create
             "kvp_cache_workspace_bytes", "kvp_cache_create", "kvp_cache_destroy", "kvp_cache_append", "kvp_cache_attend",
             "kvp_cache_copy", "kvp_cache_compact", "kvp_cache_take", "kvp_cache_share", "kvp_cache_release", "kvp_cache_fork",
             "kvp_cache_free_pages", "kvp_cache_last_error"]
+
+
+_calls = None
+
+
+def calls():
+    """The module that marshals the paged cache's calls on tensors (needs PyTorch); built like the library."""
+    global _calls
+    if _calls is None:
+        import torch  # noqa: F401  (the module's symbols are in its libraries)
+        L = lib()
+        if not os.path.exists(_build.CALLS_PATH):
+            _build.build()
+        spec = importlib.util.spec_from_file_location("_kvp_calls", _build.CALLS_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.kvp_cache_append, L.kvp_cache_attend, L.kvp_cache_compact, L.kvp_norm_rope)))
+        _calls = module
+    return _calls
 
 
 def _i32_array(xs: Sequence[int]):
@@ -465,9 +486,6 @@ def _dtype_of(t) -> int:
     return DTYPE_F32 if t.dtype == torch.float32 else DTYPE_BF16
 
 
-# The calls of a decode step take tensors every time: what is looked at is looked at once, and the arguments of an append
-# go as one packed struct (append 10.7 -> 6.7 us up to the library's call, attend 9.1 -> 3.7).
-
 def _rows(t, dtype, device: int, d: int, n: int, name: str):
     """(address, heads, token stride, head stride) of [n][head][d]."""
     shape, stride = t.shape, t.stride()
@@ -537,9 +555,17 @@ def norm_rope(q, k, positions, rope: Optional[Rope], q_out=None, k_out=None, q_w
     if first is None or first.device.type != "cuda":
         raise KvpError(1, "norm_rope: q or k on a CUDA device")
     device = first.get_device()
+    rc = calls().norm_rope(device, q, k, positions, None if rope is None else rope.address, q_out, k_out, q_weight, k_weight, eps,
+                           _raw_stream(device) if stream is None else stream.cuda_stream)
+    if rc >= 0:
+        return _checked(rc)
     a = _tokens(first.dtype, device, first.shape[-1], q, k, None, q_out, k_out, positions, None, q_weight, k_weight, eps)
     _checked(lib().kvp_norm_rope(device, _dtype_of(first), first.shape[-1], a, None if rope is None else rope.address,
                                  _raw_stream(device) if stream is None else stream.cuda_stream))
+
+
+def _closed(*args):
+    raise KvpError(4, "the cache is closed")
 
 
 class PagedCache:
@@ -577,9 +603,12 @@ class PagedCache:
             c.workspace, c.workspace_bytes = (self.workspace.data_ptr() + 255) // 256 * 256, n
         self.cfg = c
         _checked(self._L.kvp_cache_create(ctypes.byref(c), ctypes.byref(self._h)))
+        module = calls()
+        self._append, self._attend, self._compact, self._code = module.append, module.attend, module.compact, c.dtype
 
     def close(self):
         if self._h:
+            self._append = self._attend = self._compact = _closed
             if self.workspace is not None:
                 # calls on other streams may still use it; while something is recorded nothing may be waited for
                 import torch
@@ -608,6 +637,13 @@ class PagedCache:
                q_weight=None, k_weight=None, eps: float = 1e-6, stream=None):
         """q, k, v = [token][head][d] as a layer's projections give them.  Keys (normed, rotated) and values go to ``slots``
         [token] = page * page_size + row (a slot outside the store: nowhere), queries to ``q_out``."""
+        rc = self._append(self._h.value, layer, self._code, self.device, self.head_dim, k, v, positions, slots,
+                          None if rope is None else rope.address, q, q_out, k_out, q_weight, k_weight, eps, self._stream(stream))
+        if rc == 0:
+            return
+        if rc > 0:
+            self._check(rc)
+        # the tensors do not fit one another or the cache: what is wrong is found, and said, here
         if k is None or v is None or slots is None:
             raise KvpError(1, "append: k, v and slots are needed")
         a = _tokens(self.dtype, self.device, self.head_dim, q, k, v, q_out, k_out, positions, slots, q_weight, k_weight, eps)
@@ -616,6 +652,12 @@ class PagedCache:
     def attend(self, layer: int, q, table, lens, out, lse=None, first=None, stream=None):
         """q, out = [request][q head][d]; table = [request][pages], lens, first = [request], int32; lse = float32
         [request][q head].  Request b attends to its rows first[b] <= j < lens[b]."""
+        rc = self._attend(self._h.value, layer, self._code, self.device, self.head_dim, self.n_q_heads, q, out, table, lens, first, lse,
+                          self._stream(stream))
+        if rc == 0:
+            return
+        if rc > 0:
+            self._check(rc)
         n, dev, dtype, d = q.shape[0], self.device, self.dtype, self.head_dim
         qp, hq, q0, q1 = _rows(q, dtype, dev, d, n, "q")
         op, ho, o0, o1 = _rows(out, dtype, dev, d, n, "out")
@@ -638,6 +680,11 @@ class PagedCache:
     def compact(self, table, lens, new_table, kept, n_kept, stream=None):
         """Row i < n_kept[b] of new_table[b]'s pages becomes row kept[b][l][h][i] of table[b]'s; kept = [request][layer or
         1][kv head or 1][entries], int32.  The new pages must not be among those that are read."""
+        rc = self._compact(self._h.value, self.device, self.n_layers, self.n_kv_heads, table, lens, new_table, kept, n_kept, self._stream(stream))
+        if rc == 0:
+            return
+        if rc > 0:
+            self._check(rc)
         n, dev = n_kept.shape[0], self.device
         shape, stride = kept.shape, kept.stride()
         if len(shape) != 4 or shape[0] != n or kept.dtype is not _int32() or kept.get_device() != dev or (stride[3] != 1 and shape[3] > 1):

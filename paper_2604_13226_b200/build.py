@@ -1,12 +1,16 @@
-"""Builds the CUDA library in-tree: ``nvcc`` for sm_100a only, one shared object next to this file."""
+"""Builds the CUDA library in-tree: ``nvcc`` for sm_100a only, one shared object next to this file; and the Python module that
+marshals the calls of a decode step (``g++``, PyTorch's headers)."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libkvp.so")
+CALLS_PATH = os.path.join(_HERE, "_kvp_calls.so")
 SOURCES = ["kvp_api.cu", "kvp_kernels.cu", "kvp_attn_sm100.cu", "kvp_attn_pair.cu", "kvp_compose_noalloc.cu",
            "kvp_paged.cu", "kvp_paged_attn.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -14,9 +18,9 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB_PATH):
+    if not os.path.exists(LIB_PATH) or not os.path.exists(CALLS_PATH):
         return True
-    t = os.path.getmtime(LIB_PATH)
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(CALLS_PATH))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(_HERE, "..", "include", "kvp.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -39,6 +43,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB_PATH + f".{os.getpid()}.tmp"
     subprocess.check_call([nvcc, "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
     os.replace(tmp, LIB_PATH)
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    tmp = CALLS_PATH + f".{os.getpid()}.tmp"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-shared", f"-I{torch}/include",
+                           f"-I{torch}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", os.path.join(CSRC, "kvp_calls.cpp"),
+                           "-o", tmp, f"-L{torch}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, CALLS_PATH)
     return LIB_PATH
 
 

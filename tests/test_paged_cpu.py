@@ -280,3 +280,32 @@ def test_compact_arguments():
                dict(kept=i(1, 2, 2, 5)), dict(n_kept=i(3)), dict(kept=i(2, 2, 2, 10)[..., ::2]), dict(kept=i(2, 2, 2, 5).long())):
         refused(INVALID, c.compact, **dict(good, **kw))
     refused(STATE, c.compact, **good)
+
+
+def test_tensors_that_fit_go_straight_to_the_library():
+    """The module that marshals calls hands on what fits (the library then says that nothing runs here) and gives back what does
+    not; a closed cache says so."""
+    c, m = cache(heads=2, hq=4), kvp.calls()
+    t, i = (lambda *s: torch.zeros(s)), (lambda *s: torch.zeros(s, dtype=torch.int32))
+    k, q = t(3, 2, 64), t(3, 4, 64)
+    append = lambda *a: m.append(c._h.value, 0, kvp.DTYPE_F32, -1, 64, *a, 1e-6, None)
+    assert append(k, k, None, i(3), None, None, None, None, None, None) == STATE
+    assert append(k, k, i(3), i(3), kvp.Rope(64).address, q, q, k, t(64), t(64)) == STATE
+    for a in ((k, t(2, 2, 64), None, i(3), None, None, None, None, None, None), (k, k, None, i(3).long(), None, None, None, None, None, None),
+              (k, k, None, i(3), None, q, t(3, 2, 64), None, None, None), (k, 7, None, i(3), None, None, None, None, None, None),
+              (k, k, None, i(3), None, None, None, None, None, t(32)), (k.to("meta"), k, None, i(3), None, None, None, None, None, None),
+              (torch.zeros(3, 2, 64).to_sparse(), k, None, i(3), None, None, None, None, None, None)):
+        assert append(*a) == -1
+    attend = lambda *a: m.attend(c._h.value, 0, kvp.DTYPE_F32, -1, 64, 4, *a, None)
+    assert attend(q, q, i(3, 5), i(3), i(3), t(3, 4)) == STATE
+    for a in ((q, q, i(2, 5), i(3), None, None), (q, q, i(3, 5), i(3), None, t(4, 3).T), (q, q.double(), i(3, 5), i(3), None, None), (None, q, i(3, 5), i(3), None, None)):
+        assert attend(*a) == -1
+    assert m.compact(c._h.value, -1, 2, 2, i(2, 3), i(2), i(2, 2), i(2, 2, 1, 5), i(2), None) == STATE
+    assert m.compact(c._h.value, -1, 2, 2, i(2, 3), i(2), i(2, 2), i(2, 3, 1, 5), i(2), None) == -1
+    assert m.norm_rope(-1, q, None, i(3), None, q, None, None, None, 1e-6, None) == -1
+    with pytest.raises(TypeError):
+        m.append(1, 2)
+    c.close()
+    refused(STATE, c.append, 0, k, k, i(3), i(3))
+    refused(STATE, c.attend, 0, q, i(3, 5), i(3), q)
+    c.close()
