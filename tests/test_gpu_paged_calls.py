@@ -264,3 +264,37 @@ def test_appends_of_every_length(dtype, d, hq, hkv, n):
         want, tol = ref.norm_rotate(src, w, 1e-6, pos, f, 0, 1.0)
         ref.check(x, want, tol + 1.001 * ref.HALF_STEP[dtype] * want.abs())
     assert torch.equal(v[0, s // page, :, s % page], vn)
+
+
+@pytest.mark.parametrize("batch", [3, 40])
+@pytest.mark.parametrize("tokens", [1, 500, 30000])
+def test_lengths_written_by_the_call_in_front(batch, tokens):
+    """An attend may begin while the kernel in front of it ends.  Here that kernel writes its lengths - rows that norm_rope hands
+    through unchanged, whose bits are the lengths - other ones every time."""
+    page, hq, hkv, d = 16, 8, 2, 64
+    most = [900, 40, 3000] + [20] * (batch - 3)
+    n_pages = sum(-(-n // page) for n in most)
+    k, v = ref.pages((1, n_pages, hkv, page, d), "heads", torch.bfloat16, seed=1)
+    c = kvp.PagedCache(k, v, hq, max_batch=batch)
+    q = torch.randn(batch, hq, d, device="cuda").bfloat16()
+    table = table_of(most, page, n_pages)
+    sets = [most, [1] * batch, [0, 40, 2999] + [0] * (batch - 3), [900, 0, 0] + [19] * (batch - 3), [0] * batch]
+    rows, want = [], []
+    for lens in sets:
+        r = torch.zeros(tokens, 1, d, device="cuda")
+        r.view(torch.int32)[-1, 0, :batch] = ints(lens)
+        rows.append(r)
+        out = torch.empty_like(q)
+        c.attend(0, q, table, ints(lens), out)
+        want.append(out)
+        assert ref.attend(k, v, "heads", 0, q, table, lens, None, page, d ** -0.5)[0].sub(out.double()).abs().max() < 0.02
+    written = torch.zeros(tokens, 1, d, device="cuda")
+    lens = written.view(torch.int32)[-1, 0, :batch]
+    outs = [torch.empty_like(q) for _ in range(200)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        kvp.norm_rope(rows[i % 5], None, None, None, written)
+        c.attend(0, q, table, lens, out)
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        assert torch.equal(out, want[i % 5]), i
