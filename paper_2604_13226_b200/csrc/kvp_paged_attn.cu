@@ -30,7 +30,13 @@ constexpr int kStages = 3;
 constexpr int kStageBytes = 8192;          // K and V rows of a tile
 constexpr int kUnitCost = 16;              // start and end of a unit, in key tiles of one warp
 constexpr int kMinShare = 8;               // tiles that a CTA is worth starting for
-constexpr int kJoin = 8;                    // parts that are read at once when a unit is joined
+constexpr int kJoin = 8;                   // parts that are read at once when a unit is joined
+// Rows of parts that one CTA joins in the time a CTA of 4 or 8 warps takes for a tile.  A unit of t tiles in shares of s is joined
+// from t/s parts of `rows` rows, and s + t/s rows/k is least at s = sqrt(t rows/k): shares are not made shorter than that.  14/2
+// heads over 12,914 rows: 21.0 us without, 16.0 with; 16/1 over 30,000 29.5, 18.8; 28/4 over 8,000 16.3, 13.5; many or long
+// units, whose shares are longer anyway, as before.  (Half of the first: 2,785 rows 8.5 -> 8.8; half or three times the second:
+// 16/1 over 3 x 3,000-12,796 rows 15.3 -> 16.4, 16.5.)
+constexpr float kJoin4 = 11.0f, kJoin8 = 16.0f;
 
 template <typename T, int D> struct shape {
     static constexpr int kRowBytes = D * (int)sizeof(T);
@@ -152,17 +158,17 @@ template <int KEYS> struct walk {
 
 // The lengths of more than 32 requests are added up by the whole CTA, a few requests per thread.  False: the CTA has no share.
 template <int KEYS, int W>
-__device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, line &ln, walk<KEYS> &w)
+__device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, float rows_per_join, line &ln, walk<KEYS> &w)
 {
-    __shared__ int sums[W], found, found_at, found_len;
+    __shared__ int sums[W], tops[W], found, found_at, found_len;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     auto length = [&](int b) {                             // of one of a request's units
         int f;
         return (visible(a, b, f) + KEYS - 1) / KEYS + kUnitCost;
     };
-    auto cut = [&](int total) {                            // this CTA's share of the line
+    auto cut = [&](int total, int longest) {               // this CTA's share of the line, of units of that length at most
         const uint32_t ctas = max(1u, min(gridDim.x, (uint32_t)total / kMinShare));
-        ln.share = ((uint32_t)total + ctas - 1) / ctas;
+        ln.share = max(((uint32_t)total + ctas - 1) / ctas, (uint32_t)sqrtf((float)longest * rows_per_join));
         if ((uint64_t)ln.share * blockIdx.x >= (uint32_t)total) return false;
         ln.begin = (int)(ln.share * blockIdx.x);
         ln.end = (int)min((uint32_t)total, ln.begin + ln.share);
@@ -178,7 +184,7 @@ __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, l
     };
     if (a.batch <= 32) {                                   // every warp for itself: no barrier on the way to the first rows
         const int len = lane < a.batch ? length(lane) : 0, upto = scan(len * units);
-        if (!cut(__shfl_sync(0xffffffffu, upto, 31))) return false;
+        if (!cut(__shfl_sync(0xffffffffu, upto, 31), __reduce_max_sync(0xffffffffu, len))) return false;
         const int who = __ffs(__ballot_sync(0xffffffffu, ln.begin < upto)) - 1;
         const int at = __shfl_sync(0xffffffffu, upto - len * units, who), one = __shfl_sync(0xffffffffu, len, who);
         w.b = who;
@@ -188,19 +194,28 @@ __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, l
         return true;
     }
     const int per = a.batch <= 32 * W ? 1 : (a.batch + 32 * W - 1) / (32 * W), b0 = threadIdx.x * per, b1 = min(b0 + per, a.batch);
-    int mine = 0;
+    int mine = 0, top = 0;
 #pragma unroll 4
-    for (int b = b0; b < b1; ++b) mine += length(b) * units;
+    for (int b = b0; b < b1; ++b) {
+        const int len = length(b);
+        mine += len * units;
+        top = max(top, len);
+    }
     int upto = scan(mine);
-    if (lane == 31) sums[warp] = upto;
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 31) {
+        sums[warp] = upto;
+        tops[warp] = top;
+    }
     __syncthreads();
     int total = 0;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
         if (i < warp) upto += sums[i];
         total += sums[i];
+        top = max(top, tops[i]);
     }
-    if (!cut(total)) return false;
+    if (!cut(total, top)) return false;
     if (upto - mine <= ln.begin && ln.begin < upto) {      // one thread has the request that the share begins in
         int at = upto - mine;
         for (int b = b0; b < b1; ++b) {
@@ -644,7 +659,7 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
 
     line ln;
     walk<S::kKeys> w;
-    if (!find_share<S::kKeys, W>(a, units, ln, w)) return;
+    if (!find_share<S::kKeys, W>(a, units, (float)min(a.group, kUnitRows) / (W == 8 ? kJoin8 : kJoin4), ln, w)) return;
     // (Code is kept short here: a CTA of a short call runs most of it once, and instructions that are not in the cache take as
     // long as the work.)
     loader<T, D, W> ld;
