@@ -73,6 +73,18 @@ def test_attend_batches(dtype, lens):
     check_attend(k, v, "heads", hq, q, table_of(lens, page, n_pages), lens)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("hq,hkv", [(17, 1), (48, 2), (32, 1), (49, 1), (71, 1)])
+@pytest.mark.parametrize("lens", [[1], [5000], [9, 0, 0, 333, 7000, 16], [7, 300] * 150])
+def test_attend_many_heads_share_a_head(dtype, d, hq, hkv, lens):
+    """Groups wider than a warp's rows: one unit or several, of a few rows or full, inside a CTA and cut into parts."""
+    page = 16
+    n_pages = sum(-(-n // page) for n in lens) + 2
+    k, v = ref.pages((1, n_pages, hkv, page, d), "heads", DT[dtype], seed=hq)
+    q = torch.randn(len(lens), hq, d, device="cuda").to(DT[dtype])
+    check_attend(k, v, "heads", hq, q, table_of(lens, page, n_pages), lens)
+
+
 @pytest.mark.parametrize("dtype,hq", [("f32", 8), ("bf16", 8), ("bf16", 24)])
 @pytest.mark.parametrize("page", [16, 24])
 def test_attend_windows(dtype, hq, page):
