@@ -520,7 +520,8 @@ KVP_API int32_t kvp_cache_append(kvp_cache *cache, int32_t layer, const kvp_toke
 
 /*
  * Attention of one new token per request over its rows first[b] <= j < lens[b] of `layer` (its own row among them, once
- * appended): softmax in fp32, q head h reads kv head h / (Hq/Hkv).
+ * appended): softmax in fp32, q head h reads kv head h / (Hq/Hkv).  bf16 probabilities meet the values as two numbers, rounded and
+ * remainder, so that an infinite value in a visible row gives NaN; rows that are not visible are never read.
  *   q      device, {batch, head} strides in elements; out likewise.  16-byte aligned, strides multiples of 16 bytes
  *   table  device [batch][table_cols] with row stride table_stride: page numbers; n_kv_heads * batch * (table_cols *
  *          page_size / 8 + 17), for groups of more than 8 heads once for each 8, is below 2^31
