@@ -544,14 +544,16 @@ bool rows_fit(const kvp_cache_config *c)
     return bytes / (double)(1ull << unit_shift_of(c)) < 4294967296.0;
 }
 
-struct cache_layout { uint64_t o, ml, arrived, total; int32_t units; };
+struct cache_layout { uint64_t o, ml, arrived, arrived_group, counted, total; int32_t units; };
 cache_layout layout_of(const kvp_cache_config *c, int32_t sm_count)
 {
     cache_layout l;
     const int64_t group = c->n_q_heads / c->n_kv_heads, slots = 2ll * kvp_paged_ctas(sm_count);
     l.units = (int32_t)std::min<int64_t>(INT32_MAX, (int64_t)c->max_batch * c->n_kv_heads * ((group + KVP_PAGED_LEAST_ROWS - 1) / KVP_PAGED_LEAST_ROWS));
     l.arrived = 0;
-    l.ml = (4ull * l.units + 255) / 256 * 256;
+    l.arrived_group = l.arrived + 4ull * l.units;
+    l.counted = l.arrived_group + 4ull * slots;            // end of what is zero between launches
+    l.ml = (l.counted + 255) / 256 * 256;
     l.o = l.ml + 8ull * slots * KVP_PAGED_ROWS;
     l.total = l.o + 4ull * slots * KVP_PAGED_ROWS * c->head_dim;
     return l;
@@ -774,11 +776,11 @@ int32_t kvp_cache_create(const kvp_cache_config *cfg, kvp_cache **out)
         if (cfg->workspace_bytes < layout_of(cfg, kMostSms).total) return bail(fail(nullptr, KVP_ERR_CAPACITY, "cache_create: workspace too small"));
         const cache_layout l = layout_of(cfg, kMostSms);
         char *ws = (char *)cfg->workspace;
-        c->ws = {(float *)(ws + l.o), (float2 *)(ws + l.ml), (int32_t *)(ws + l.arrived)};
+        c->ws = {(float *)(ws + l.o), (float2 *)(ws + l.ml), (int32_t *)(ws + l.arrived), (int32_t *)(ws + l.arrived_group)};
         if (e == cudaSuccess) e = kvp_paged_attn_prepare(cfg->dtype, cfg->head_dim);
         // whatever is still under way on this memory, on any stream, before it becomes the cache's
         if (e == cudaSuccess) e = cudaDeviceSynchronize();
-        if (e == cudaSuccess) e = cudaMemsetAsync(c->ws.arrived, 0, 4ull * l.units, 0);
+        if (e == cudaSuccess) e = cudaMemsetAsync(ws, 0, l.counted, 0);
         if (e == cudaSuccess) e = cudaStreamSynchronize(0);
         if (e != cudaSuccess) return bail(cuda_failed(nullptr, "cache_create", e));
     }

@@ -53,6 +53,7 @@ struct kvp_paged_ws {
     float *part_o;             // [2 * CTAs][16][head_dim]
     float2 *part_ml;           // [2 * CTAs][16]
     int32_t *arrived;          // [units], zero between launches
+    int32_t *arrived_group;    // [2 * CTAs], by a group's first part; likewise
 };
 
 struct kvp_paged_args {

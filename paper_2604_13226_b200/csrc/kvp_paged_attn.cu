@@ -12,6 +12,7 @@
 //   lengths as they lie in device memory, so that a captured launch follows them.
 // * A unit inside one CTA is written out by it.  The parts of a unit that several CTAs share go to the workspace, and the CTA
 //   whose part is the last to arrive joins them, always in the order of the parts: results do not depend on who came last.
+//   Dozens of parts are joined in two steps, groups of neighbours first.
 // * Inside a CTA every warp streams key tiles of its own (one in 4 or 8 of the CTA's) through a ring of cp.async stages, without
 //   any barrier; the warps' running maxima, sums and outputs are joined in shared memory at a unit's end.  The ring runs on
 //   into the next unit meanwhile.
@@ -31,11 +32,16 @@ constexpr int kStageBytes = 8192;          // K and V rows of a tile
 constexpr int kUnitCost = 16;              // start and end of a unit, in key tiles of one warp
 constexpr int kMinShare = 8;               // tiles that a CTA is worth starting for
 constexpr int kJoin = 8;                   // parts that are read at once when a unit is joined
+// Units of more than kFlat parts are joined in groups of kGroup first, groups at the same time; eight parts take 0.4 us, the
+// second step 1.7.  One request of 54,000 rows: 28/4 heads 35.7 -> 29.0 us, 16/1 23.5 -> 18.3, 133,120 of 8/2
+// 38.8 -> 31.2.  (kFlat 12: 2,785 rows 8.7 -> 9.6; 22: 9.5; kGroup 12, 16/1 18.3 -> 19.5.)
+constexpr int kGroup = 8, kFlat = 30;
 // Rows of parts that one CTA joins in the time a CTA of 4 or 8 warps takes for a tile.  A unit of t tiles in shares of s is joined
-// from t/s parts of `rows` rows, and s + t/s rows/k is least at s = sqrt(t rows/k): shares are not made shorter than that.  14/2
-// heads over 12,914 rows: 21.0 us without, 16.0 with; 16/1 over 30,000 29.5, 18.8; 28/4 over 8,000 16.3, 13.5; many or long
-// units, whose shares are longer anyway, as before.  (Half of the first: 2,785 rows 8.5 -> 8.8; half or three times the second:
-// 16/1 over 3 x 3,000-12,796 rows 15.3 -> 16.4, 16.5.)
+// from t/s parts of `rows` rows, and s + t/s rows/k is least at s = sqrt(t rows/k): shares are not made shorter than that - or
+// than half of it, where that leaves so many parts that they are joined in groups (16/1 heads over 54,000 rows: the whole 20.6
+// us, 0.7 19.7, a half 18.5, a third 19.2).  28/4 heads over 8,000 rows: 16.3 us without, 13.9 with; many or long units, whose
+// shares are longer anyway, as before.  (Half of the first: 2,785 rows 8.5 -> 8.8; half or three times the second: 16/1 over
+// 3 x 3,000-12,796 rows 15.3 -> 16.4, 16.5.)
 constexpr float kJoin4 = 11.0f, kJoin8 = 16.0f;
 
 template <typename T, int D> struct shape {
@@ -168,7 +174,10 @@ __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, f
     };
     auto cut = [&](int total, int longest) {               // this CTA's share of the line, of units of that length at most
         const uint32_t ctas = max(1u, min(gridDim.x, (uint32_t)total / kMinShare));
-        ln.share = max(((uint32_t)total + ctas - 1) / ctas, (uint32_t)sqrtf((float)longest * rows_per_join));
+        const uint32_t even = ((uint32_t)total + ctas - 1) / ctas;
+        const float least = sqrtf((float)longest * rows_per_join);
+        ln.share = max(even, (uint32_t)least);
+        if ((uint32_t)longest / kFlat >= ln.share) ln.share = max(even, (uint32_t)(least * 0.5f));
         if ((uint64_t)ln.share * blockIdx.x >= (uint32_t)total) return false;
         ln.begin = (int)(ln.share * blockIdx.x);
         ln.end = (int)min((uint32_t)total, ln.begin + ln.share);
@@ -727,54 +736,70 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
                 // whoever's part is the last joins them
                 const int t0 = p.at + kUnitCost;
                 const int c0 = ln.owner(t0), n_parts = ln.owner(t0 + tiles - 1) - c0 + 1;
-                int32_t *arrived = a.ws.arrived + p.b * units + p.u;
-                // (a barrier lies behind the parts' stores: thread 0's release covers all of them, and its acquire what others released)
-                if (threadIdx.x == 0) {
-                    int before;
-                    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(arrived) : "memory");
-                    last = before == n_parts - 1;
-                    if (last) *arrived = 0;
-                }
-                __syncthreads();
-                if (!last) return;
-                // D/4 threads take a row, four columns each; each of them first weighs one part, then all add up kJoin parts at a time
-                constexpr int L = D / 4;
-                for (int x = threadIdx.x; x - (int)threadIdx.x % 32 < n_rows * L; x += 32 * W) {
-                    const int r = min(x / L, n_rows - 1), c4 = x % L;
-                    const int row0 = 2 * c0 * KVP_PAGED_ROWS + r;          // of part p, p > 0: this + 2 p rows; of part 0 one slot on
-                    auto part = [&](int i) { return row0 + (i == 0 ? 1 : 2 * i) * KVP_PAGED_ROWS; };
-                    float m = -INFINITY, l = 0.0f;
-                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    for (int p0 = 0; p0 < n_parts; p0 += L) {
-                        const int n = min(L, n_parts - p0);
-                        const float2 ml = c4 < n ? __ldcg(a.ws.part_ml + part(p0 + c4)) : make_float2(-INFINITY, 0.0f);
-                        float weight = 0.0f;
-                        for (int k0 = 0; k0 < n; k0 += kJoin) {
-                            float4 y[kJoin];
+                auto slot_of = [&](int i) { return 2 * (c0 + i) + (i == 0); };
+#pragma unroll 1
+                for (bool inner = n_parts > kFlat;; inner = false) {
+                    int step = !inner && n_parts > kFlat ? kGroup : 1;
+                    asm volatile("" : "+r"(step));         // one join for both: made twice, it cost fp32 of 14/2 heads 4 %
+                    const int i0 = inner ? ((int)blockIdx.x - c0) / kGroup * kGroup : 0;
+                    const int count = inner ? min(kGroup, n_parts - i0) : (n_parts + step - 1) / step;     // parts i0, i0 + step, ...
+                    // (a barrier lies behind the parts' stores: thread 0's release covers all of them, and its acquire what others released)
+                    if (threadIdx.x == 0) {
+                        int32_t *arrived = inner ? a.ws.arrived_group + slot_of(i0) : a.ws.arrived + p.b * units + p.u;
+                        int before;
+                        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(arrived) : "memory");
+                        last = before == count - 1;
+                        if (last) *arrived = 0;
+                    }
+                    __syncthreads();
+                    if (!last) return;
+                    // D/4 threads take a row, four columns each; each of them first weighs one part, then all add up kJoin parts at a time
+                    constexpr int L = D / 4;
+                    for (int x = threadIdx.x; x - (int)threadIdx.x % 32 < n_rows * L; x += 32 * W) {
+                        const int r = min(x / L, n_rows - 1), c4 = x % L;
+                        const int row0 = 2 * (c0 + i0) * KVP_PAGED_ROWS + r, row1 = 2 * step * KVP_PAGED_ROWS;
+                        auto part = [&](int i) { return row0 + (i > 0 ? i * row1 : i0 == 0 ? KVP_PAGED_ROWS : 0); };
+                        float m = -INFINITY, l = 0.0f;
+                        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        for (int p0 = 0; p0 < count; p0 += L) {
+                            const int n = min(L, count - p0);
+                            const float2 ml = c4 < n ? __ldcg(a.ws.part_ml + part(p0 + c4)) : make_float2(-INFINITY, 0.0f);
+                            float weight = 0.0f;
+                            for (int k0 = 0; k0 < n; k0 += kJoin) {
+                                float4 y[kJoin];
 #pragma unroll
-                            for (int k = 0; k < kJoin; ++k) y[k] = __ldcg(reinterpret_cast<const float4 *>(a.ws.part_o + part(p0 + min(k0 + k, n - 1)) * D) + c4);
-                            if (k0 == 0) {
-                                float top = ml.x;
+                                for (int k = 0; k < kJoin; ++k) y[k] = __ldcg(reinterpret_cast<const float4 *>(a.ws.part_o + part(p0 + min(k0 + k, n - 1)) * D) + c4);
+                                if (k0 == 0) {
+                                    float top = ml.x;
 #pragma unroll
-                                for (int w = L / 2; w > 0; w /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-                                top = fmaxf(top, m);
-                                const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(m - ref);
-                                m = top;
-                                weight = exp2_fast(ml.x - ref);
-                                float sum = weight * ml.y;
+                                    for (int w = L / 2; w > 0; w /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                                    top = fmaxf(top, m);
+                                    const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(m - ref);
+                                    m = top;
+                                    weight = exp2_fast(ml.x - ref);
+                                    float sum = weight * ml.y;
 #pragma unroll
-                                for (int w = L / 2; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-                                o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
-                                l = l * f0 + sum;
-                            }
+                                    for (int w = L / 2; w > 0; w /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                                    o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+                                    l = l * f0 + sum;
+                                }
 #pragma unroll
-                            for (int k = 0; k < kJoin; ++k) {
-                                const float f = __shfl_sync(0xffffffffu, weight, (k0 + k) % L, L);
-                                if (k0 + k < n) { o.x += f * y[k].x; o.y += f * y[k].y; o.z += f * y[k].z; o.w += f * y[k].w; }
+                                for (int k = 0; k < kJoin; ++k) {
+                                    const float f = __shfl_sync(0xffffffffu, weight, (k0 + k) % L, L);
+                                    if (k0 + k < n) { o.x += f * y[k].x; o.y += f * y[k].y; o.z += f * y[k].z; o.w += f * y[k].w; }
+                                }
                             }
                         }
+                        if (x >= n_rows * L) continue;
+                        if (inner) {                                   // in the place of the group's first part
+                            reinterpret_cast<float4 *>(a.ws.part_o + part(0) * D)[c4] = o;
+                            if (c4 == 0) a.ws.part_ml[part(0)] = make_float2(m, l);
+                        } else {
+                            write_row<T, D>(a, p.b, head0 + r, c4, o, m, l);
+                        }
                     }
-                    if (x < n_rows * L) write_row<T, D>(a, p.b, head0 + r, c4, o, m, l);
+                    if (!inner) return;
+                    __syncthreads();
                 }
             }();
         }

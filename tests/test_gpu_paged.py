@@ -85,6 +85,25 @@ def test_attend_many_heads_share_a_head(dtype, d, hq, hkv, lens):
     check_attend(k, v, "heads", hq, q, table_of(lens, page, n_pages), lens)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (7, 1), (16, 1), (20, 1), (28, 4)])
+@pytest.mark.parametrize("lens", [[60000], [30001, 3, 0, 9000, 17000]])
+def test_attend_units_of_many_parts(dtype, d, hq, hkv, lens):
+    """Units that dozens of CTAs share, joined in groups of parts first; twice on one cache, the second time the same."""
+    page = 64
+    n_pages = sum(-(-n // page) for n in lens) + 2
+    k, v = ref.pages((1, n_pages, hkv, page, d), "tokens", DT[dtype], seed=hq)
+    q = torch.randn(len(lens), hq, d, device="cuda").to(DT[dtype])
+    table = table_of(lens, page, n_pages)
+    out, lse = check_attend(k, v, "tokens", hq, q, table, lens)
+    c = kvp.PagedCache(k, v, hq, order="tokens", max_batch=len(lens))
+    for _ in range(2):
+        again, lse_again = torch.empty_like(out), torch.empty_like(lse)
+        c.attend(0, q, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), out=again, lse=lse_again)
+        assert torch.equal(again, out) and torch.equal(lse_again, lse)
+    c.close()
+
+
 @pytest.mark.parametrize("dtype,hq", [("f32", 8), ("bf16", 8), ("bf16", 24)])
 @pytest.mark.parametrize("page", [16, 24])
 def test_attend_windows(dtype, hq, page):
