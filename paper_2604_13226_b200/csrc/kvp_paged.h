@@ -22,6 +22,12 @@ struct kvp_store {
     kvp_divisor by_page;
 };
 
+// Key tiles of `rows` rows, 0 to 2^31 - 1 of them (rounded up in 32 bits: the sum may pass 2^31).
+#ifdef __CUDACC__
+__host__ __device__
+#endif
+constexpr int32_t kvp_tiles(int32_t rows, int32_t keys) { return (int32_t)(((uint32_t)rows + (uint32_t)keys - 1) / (uint32_t)keys); }
+
 #ifdef __CUDACC__
 __device__ __forceinline__ int32_t divide(int32_t n, kvp_divisor d) { return (int32_t)(((uint64_t)(uint32_t)n * d.mul) >> d.shift); }
 

@@ -138,7 +138,7 @@ template <int KEYS> struct walk {
     {
         if (b >= a.batch) return;
         rows = visible(a, b, first);
-        tiles = (rows + KEYS - 1) / KEYS;
+        tiles = kvp_tiles(rows, KEYS);
     }
     // To the next unit with something to do for this CTA.  False: there is none.
     __device__ bool next(const kvp_paged_args &a, const line &ln, int units, piece &p)
@@ -170,7 +170,7 @@ __device__ __forceinline__ bool find_share(const kvp_paged_args &a, int units, f
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     auto length = [&](int b) {                             // of one of a request's units
         int f;
-        return (visible(a, b, f) + KEYS - 1) / KEYS + kUnitCost;
+        return kvp_tiles(visible(a, b, f), KEYS) + kUnitCost;
     };
     auto cut = [&](int total, int longest) {               // this CTA's share of the line, of units of that length at most
         const uint32_t ctas = max(1u, min(gridDim.x, (uint32_t)total / kMinShare));
@@ -285,10 +285,11 @@ template <typename T, int D, int W> struct loader {
         x.page = -2;
         if (tile >= p.hi) next_piece(a, ln, units);
         if (!more) return;
-        const int lane = threadIdx.x % 32, i = tile * S::kKeys + lane;
+        const int lane = threadIdx.x % 32;
+        const uint32_t i = (uint32_t)(tile * S::kKeys) + lane;     // (a last tile may reach beyond 2^31)
         x.page = -1;
-        if (lane < S::kKeys && i < p.rows) {
-            const int r = p.first + i, col = divide(r, a.st.by_page);
+        if (lane < S::kKeys && i < (uint32_t)p.rows) {
+            const int r = p.first + (int)i, col = divide(r, a.st.by_page);
             x.row = r - col * a.st.page_size;
             x.head = p.u / row_tiles;
             x.page = a.table[p.b * a.table_stride + col];
@@ -694,7 +695,7 @@ paged_attn_kernel(const __grid_constant__ kvp_paged_args a)
             const int rt = p.u % row_tiles * kUnitRows, head0 = p.u / row_tiles * a.group + rt, n_rows = min(kUnitRows, a.group - rt);
             [&]() {
                 // the warps' parts, 8 rows at a time; a thread has 4 columns of a row
-                const int tiles = (p.rows + S::kKeys - 1) / S::kKeys;
+                const int tiles = kvp_tiles(p.rows, S::kKeys);
                 const bool whole = p.lo == 0 && p.hi == tiles;
                 const int slot = 2 * blockIdx.x + (p.lo > 0 ? 0 : 1);
                 // (groups of up to four, whose units are all alike, take the two halves of the space in turn, and need no barrier

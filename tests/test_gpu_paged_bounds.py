@@ -1,0 +1,40 @@
+"""The paged cache's calls at the ends of their ranges on the GPU."""
+import math
+
+import pytest
+import torch
+
+import paged_reference as ref
+from paper_2604_13226_b200 import binding as kvp
+from test_gpu_paged import ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64), (torch.float32, 128)])
+@pytest.mark.parametrize("hq", [1, 20])
+@pytest.mark.parametrize("short", [1, 31, 33])
+def test_the_longest_lengths(dtype, d, hq, short):
+    """Lengths within a tile of 2^31 over lists of absent pages: only the first and the last one are there."""
+    page, cols = 64, 1 << 25
+    k, v = ref.pages((1, 3, 1, page, d), "heads", dtype, seed=d + hq)
+    c = kvp.PagedCache(k, v, hq, max_batch=2)
+    g = torch.Generator(device="cuda").manual_seed(hq)
+    q = torch.randn(2, hq, d, generator=g, device="cuda").to(dtype)
+    table = torch.full((2, cols), -1, dtype=torch.int32, device="cuda")
+    table[0, 0], table[0, -1], table[1, 0] = 2, 0, 1
+    out, lse = torch.full_like(q, 7.0), torch.full((2, hq), 7.0, device="cuda")
+    lens = [2 ** 31 - short, 5]
+    c.attend(0, q, table, ints(lens), out, lse=lse, first=ints([10, 0]))
+    want = ref.attend(k, v, "heads", 0, q, ints([[2, 0], [1, -1]]), [2 * page - short, 5], [10, 0], page, d ** -0.5)
+    ref.check(out, want[0], want[2], "out")
+    ref.check(lse, want[1], want[3], "lse")
+    if short == 1:                                                 # a list that ends later than lengths can say
+        wide = torch.full((1, cols + 9), -1, dtype=torch.int32, device="cuda")
+        wide[0, :cols] = table[0]
+        again = torch.full_like(out[:1], 7.0)
+        c.attend(0, q[:1], wide, ints(lens[:1]), again, first=ints([10]))
+        ref.check(again, want[0][:1], want[2][:1], "out")
+        nothing = torch.full_like(out[:1], 7.0)
+        c.attend(0, q[:1], torch.full_like(wide, 3), ints(lens[:1]), nothing, lse=lse[:1])
+        assert not nothing.any() and bool((lse[0] == -math.inf).all())

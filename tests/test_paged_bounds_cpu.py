@@ -1,0 +1,23 @@
+"""The paged cache's calls at the ends of their ranges, and what surrounds them, without a GPU."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2604_13226_b200 import binding as kvp
+from paper_2604_13226_b200 import build
+from test_paged_cpu import CAPACITY, INVALID, STATE, cache, refused
+
+
+def test_tiles_of_the_longest_lists(tmp_path):
+    """Rows are cut into tiles without the count passing 31 bits, whatever the length."""
+    src = tmp_path / "tiles.cpp"
+    src.write_text(f'#include "{build.CSRC}/kvp_paged.h"\nextern "C" int32_t tiles(int32_t rows, int32_t keys) {{ return kvp_tiles(rows, keys); }}\n')
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O1", "-std=c++17", "-fPIC", "-shared", "-fwrapv", f"-I{cuda}/include", str(src), "-o", str(tmp_path / "tiles.so")])
+    tiles = ctypes.CDLL(str(tmp_path / "tiles.so")).tiles
+    for keys in (8, 16, 32):
+        for rows in [*range(100), *range(2 ** 30 - 40, 2 ** 30 + 40), *range(2 ** 31 - 100, 2 ** 31)]:
+            assert tiles(rows, keys) == -(-rows // keys), (rows, keys)
