@@ -548,7 +548,7 @@ KVP_API int32_t kvp_cache_copy(kvp_cache *cache, int32_t n, const int32_t *src, 
  * layer l and kv head h, K and V.  Keys keep the rotation of the position they were cached at, so each head may keep rows of
  * its own; later tokens go on at positions of the caller's (kvp_tokens.positions).
  *   kept      device, strides kept_stride = {request, layer, head} in elements (0: the same list for all), max_kept entries
- *   n_kept    device [batch], at most max_kept
+ *   n_kept    device [batch], at most max_kept; below 0 is none
  * A kept row at or behind lens[b], or on a page outside the store, leaves its place as it is.  The pages of new_table must
  * not be among those that are read.  Errors: INVALID, STATE (host only), CUDA.
  */

@@ -409,8 +409,9 @@ compact_kernel(const __grid_constant__ compact_args a)
     pdl_launch_dependents();
     pdl_wait();
     const int b = blockIdx.z, layer = blockIdx.y / a.n_kv, h = blockIdx.y % a.n_kv, i0 = blockIdx.x * kCompactRows;
-    const int n = min(min(a.n_kept[b], a.max_kept) - i0, kCompactRows);
-    if (n <= 0) return;
+    const int end = min(a.n_kept[b], a.max_kept);
+    if (end <= i0) return;                         // (before anything is subtracted: n_kept may be any number)
+    const int n = min(end - i0, kCompactRows);
     if ((int)threadIdx.x < n) {
         const int i = i0 + threadIdx.x, new_page = divide(i, a.st.by_page);
         const int dst = new_page < a.new_cols ? a.new_table[b * a.new_stride + new_page] : -1;

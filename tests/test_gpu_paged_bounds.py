@@ -38,3 +38,19 @@ def test_the_longest_lengths(dtype, d, hq, short):
         nothing = torch.full_like(out[:1], 7.0)
         c.attend(0, q[:1], torch.full_like(wide, 3), ints(lens[:1]), nothing, lse=lse[:1])
         assert not nothing.any() and bool((lse[0] == -math.inf).all())
+
+
+def test_compact_with_counts_below_zero():
+    """A count below zero, the lowest number too, keeps nothing: not a row of the later blocks either."""
+    k, v = ref.pages((2, 40, 2, 16, 64), "heads", torch.bfloat16, seed=1)
+    was = k.clone(), v.clone()
+    c = kvp.PagedCache(k, v, 4)
+    counts = [-2 ** 31, -2 ** 31 + 31, -1, 0, 35]
+    table = torch.arange(20, dtype=torch.int32, device="cuda").view(5, 4)
+    kept = torch.arange(60, dtype=torch.int32, device="cuda").add(2).expand(5, 1, 1, 60).contiguous()
+    c.compact(table, ints([64] * 5), table + 20, kept, ints(counts))
+    torch.cuda.synchronize()
+    for t, w in ((k, was[0]), (v, was[1])):
+        for i in range(35):
+            w[:, 36 + i // 16, :, i % 16] = w[:, 16 + (i + 2) // 16, :, (i + 2) % 16]
+        assert torch.equal(t, w)
