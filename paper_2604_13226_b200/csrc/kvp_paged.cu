@@ -892,7 +892,7 @@ int32_t kvp_cache_compact(kvp_cache *c, int32_t batch, const int32_t *table, int
     if (batch < 0 || batch > 65535 || table_cols < 0 || new_cols < 0 || max_kept < 0) return fail(c, KVP_ERR_INVALID, "compact: bad count");
     const bool any = batch > 0 && max_kept > 0;
     if (any) {
-        if (!table || !lens || !new_table || !kept || !kept_stride || !n_kept) return fail(c, KVP_ERR_INVALID, "compact: null pointer");
+        if ((!table && table_cols > 0) || (!new_table && new_cols > 0) || !lens || !kept || !kept_stride || !n_kept) return fail(c, KVP_ERR_INVALID, "compact: null pointer");
         if (((uintptr_t)table | (uintptr_t)lens | (uintptr_t)new_table | (uintptr_t)kept | (uintptr_t)n_kept) & 3)
             return fail(c, KVP_ERR_INVALID, "compact: arrays must be aligned");
         if (llabs(table_stride) > (1ll << 56) || llabs(new_stride) > (1ll << 56)) return fail(c, KVP_ERR_INVALID, "compact: strides");

@@ -54,3 +54,18 @@ def test_compact_with_counts_below_zero():
         for i in range(35):
             w[:, 36 + i // 16, :, i % 16] = w[:, 16 + (i + 2) // 16, :, (i + 2) % 16]
         assert torch.equal(t, w)
+
+
+def test_compaction_of_tables_without_columns():
+    """Nothing is kept, or nothing is there to be kept: rows stay as they are."""
+    k, v = ref.pages((2, 12, 2, 16, 64), "heads", torch.bfloat16, seed=2)
+    was = k.clone(), v.clone()
+    c = kvp.PagedCache(k, v, 4)
+    i = lambda *n: torch.empty(n, dtype=torch.int32, device="cuda")
+    table, kept = ints([[0, 1], [2, 3]]), torch.arange(20, dtype=torch.int32, device="cuda").expand(2, 1, 1, 20)
+    c.compact(table, ints([30, 30]), i(2, 0), kept, ints([0, 0]))
+    c.compact(table, ints([30, 30]), i(2, 0), kept, ints([20, 3]))
+    c.compact(i(2, 0), ints([30, 30]), table + 4, kept, ints([20, 3]))
+    c.compact(i(2, 0), ints([30, 0]), i(2, 0), kept, ints([20, 3]))
+    torch.cuda.synchronize()
+    assert torch.equal(k, was[0]) and torch.equal(v, was[1])

@@ -21,3 +21,15 @@ def test_tiles_of_the_longest_lists(tmp_path):
     for keys in (8, 16, 32):
         for rows in [*range(100), *range(2 ** 30 - 40, 2 ** 30 + 40), *range(2 ** 31 - 100, 2 ** 31)]:
             assert tiles(rows, keys) == -(-rows // keys), (rows, keys)
+
+
+def test_compaction_of_tables_without_columns():
+    """Requests that keep nothing have no new pages, and those without rows no old ones: tables of [n][0] have no address."""
+    c = cache(layers=2, heads=2)
+    i = lambda *n: torch.zeros(n, dtype=torch.int32)
+    good = dict(table=i(2, 3), lens=i(2), new_table=i(2, 2), kept=i(2, 1, 1, 5), n_kept=i(2))
+    for kw in (dict(new_table=i(2, 0)), dict(table=i(2, 0)), dict(table=i(2, 0), new_table=i(2, 0))):
+        refused(STATE, c.compact, **dict(good, **kw))              # it would run where something runs
+    one, zero = (ctypes.c_int32 * 8)(), (ctypes.c_int64 * 3)()
+    call = lambda table, cols, new, new_cols: kvp.lib().kvp_cache_compact(c._h, 2, table, 4, cols, one, new, 4, new_cols, one, zero, 1, one, None)
+    assert call(None, 0, None, 0) == STATE and call(None, 1, one, 1) == INVALID and call(one, 1, None, 1) == INVALID
