@@ -6,6 +6,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <type_traits>
+
 #include <ATen/core/TensorBase.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -29,8 +31,10 @@ bool on_device(const at::Tensor &t, int device)
     return device < 0 ? t.is_cpu() : t.is_cuda() && t.get_device() == device;
 }
 
-// [n][heads][d]; n < 0, heads < 0: any, and told
-bool rows(PyObject *o, const wanted &w, int64_t &n, int64_t &heads, const void *&p, int64_t *stride)
+// [n][heads][d]; n < 0, heads < 0: any, and told.  Written to where p is not const (a lazily cloned tensor then gets memory of its own:
+// outputs are asked for in front of inputs, so that one that is both has one address).
+template <typename P>
+bool rows(PyObject *o, const wanted &w, int64_t &n, int64_t &heads, P *&p, int64_t *stride)
 {
     if (!THPVariable_Check(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
@@ -39,7 +43,8 @@ bool rows(PyObject *o, const wanted &w, int64_t &n, int64_t &heads, const void *
     if ((n >= 0 && size[0] != n) || (heads >= 0 && size[1] != heads) || size[2] != w.d || step[2] != 1) return false;
     n = size[0];
     heads = size[1];
-    p = t.const_data_ptr();
+    if constexpr (std::is_const_v<P>) p = t.const_data_ptr();
+    else p = t.mutable_data_ptr();
     stride[0] = step[0];
     stride[1] = step[1];
     return true;
@@ -100,14 +105,11 @@ PyObject *append(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     int64_t n = -1, hq = -1, hkv = -1;
     bool fits = true;
     try {
-        const void *q_out = nullptr, *k_out = nullptr;
-        fits = rows(args[5], w, n, hkv, t.k, t.k_stride) && rows(args[6], w, n, hkv, t.v, t.v_stride) && n <= INT32_MAX && hkv <= INT32_MAX &&
+        fits = (!given(args[11]) || rows(args[11], w, n, hq, t.q_out, t.q_out_stride)) && (!given(args[12]) || rows(args[12], w, n, hkv, t.k_out, t.k_out_stride)) &&
+               rows(args[5], w, n, hkv, t.k, t.k_stride) && rows(args[6], w, n, hkv, t.v, t.v_stride) && n <= INT32_MAX && hkv <= INT32_MAX &&
                (!given(args[7]) || ints(args[7], w.device, n, t.positions)) && ints(args[8], w.device, n, t.slots) &&
-               (!given(args[10]) || rows(args[10], w, n, hq, t.q, t.q_stride)) && (!given(args[11]) || rows(args[11], w, n, hq, q_out, t.q_out_stride)) &&
-               hq <= INT32_MAX && (!given(args[12]) || rows(args[12], w, n, hkv, k_out, t.k_out_stride)) &&
+               (!given(args[10]) || rows(args[10], w, n, hq, t.q, t.q_stride)) && hq <= INT32_MAX &&
                (!given(args[13]) || vector_of(args[13], w, t.q_weight)) && (!given(args[14]) || vector_of(args[14], w, t.k_weight));
-        t.q_out = const_cast<void *>(q_out);
-        t.k_out = const_cast<void *>(k_out);
     } catch (...) {                                // a tensor without memory, say
         fits = false;
     }
@@ -129,12 +131,13 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     int64_t hq = PyLong_AsLong(args[5]), n = -1, cols = 0, table_stride = 0, q_stride[2], out_stride[2];
     void *stream = given(args[12]) ? PyLong_AsVoidPtr(args[12]) : nullptr;
     if (PyErr_Occurred()) return nullptr;
-    const void *q = nullptr, *out = nullptr;
+    const void *q = nullptr;
+    void *out = nullptr;
     const int32_t *table = nullptr, *lens = nullptr, *first = nullptr;
     float *lse = nullptr;
     bool fits = true;
     try {
-        fits = rows(args[6], w, n, hq, q, q_stride) && rows(args[7], w, n, hq, out, out_stride) && n <= INT32_MAX &&
+        fits = rows(args[7], w, n, hq, out, out_stride) && rows(args[6], w, n, hq, q, q_stride) && n <= INT32_MAX &&
                ints(args[8], w.device, n, table, &cols, &table_stride) && cols <= INT32_MAX && ints(args[9], w.device, n, lens) &&
                (!given(args[10]) || ints(args[10], w.device, n, first));
         if (fits && given(args[11])) {
@@ -150,7 +153,7 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     }
     if (!fits) return PyLong_FromLong(-1);
     return PyLong_FromLong(g_attend((kvp_cache *)handle, layer, (int32_t)n, q, q_stride, table, table_stride, (int32_t)cols, lens, first,
-                                    const_cast<void *>(out), out_stride, lse, stream));
+                                    out, out_stride, lse, stream));
 }
 
 // (cache, device, layers, kv heads, table, lens, new_table, kept, n_kept, stream) -> status
@@ -211,13 +214,10 @@ PyObject *norm_rope(PyObject *, PyObject *const *args, Py_ssize_t n_args)
             w.d = f.dim() == 3 ? f.size(2) : -1;
             fits = w.type == c10::kFloat || w.type == c10::kBFloat16;
         }
-        const void *q_out = nullptr, *k_out = nullptr;
-        fits = fits && (!given(args[1]) || rows(args[1], w, n, hq, t.q, t.q_stride)) && (!given(args[2]) || rows(args[2], w, n, hkv, t.k, t.k_stride)) &&
+        fits = fits && (!given(args[5]) || rows(args[5], w, n, hq, t.q_out, t.q_out_stride)) && (!given(args[6]) || rows(args[6], w, n, hkv, t.k_out, t.k_out_stride)) &&
+               (!given(args[1]) || rows(args[1], w, n, hq, t.q, t.q_stride)) && (!given(args[2]) || rows(args[2], w, n, hkv, t.k, t.k_stride)) &&
                n <= INT32_MAX && hq <= INT32_MAX && hkv <= INT32_MAX && w.d <= INT32_MAX && (!given(args[3]) || ints(args[3], w.device, n, t.positions)) &&
-               (!given(args[5]) || rows(args[5], w, n, hq, q_out, t.q_out_stride)) && (!given(args[6]) || rows(args[6], w, n, hkv, k_out, t.k_out_stride)) &&
                (!given(args[7]) || vector_of(args[7], w, t.q_weight)) && (!given(args[8]) || vector_of(args[8], w, t.k_weight));
-        t.q_out = const_cast<void *>(q_out);
-        t.k_out = const_cast<void *>(k_out);
     } catch (...) {
         fits = false;
     }

@@ -33,3 +33,21 @@ def test_compaction_of_tables_without_columns():
     one, zero = (ctypes.c_int32 * 8)(), (ctypes.c_int64 * 3)()
     call = lambda table, cols, new, new_cols: kvp.lib().kvp_cache_compact(c._h, 2, table, 4, cols, one, new, 4, new_cols, one, zero, 1, one, None)
     assert call(None, 0, None, 0) == STATE and call(None, 1, one, 1) == INVALID and call(one, 1, None, 1) == INVALID
+
+
+def test_outputs_are_separated_from_what_they_were_cloned_from():
+    """A lazily cloned output has its original's memory until something asks to write to it: taking its address does."""
+    lazy = getattr(torch, "_lazy_clone", None)
+    if lazy is None:
+        pytest.skip("this PyTorch has no lazy clones")
+    c, rope = cache(heads=2, hq=4), kvp.Rope(64)
+    t, i = (lambda *s: torch.zeros(s)), (lambda *s: torch.zeros(s, dtype=torch.int32))
+    k, q = t(3, 2, 64), t(3, 4, 64)
+    outs = [lazy(q), lazy(k), lazy(q), lazy(t(3, 4))]
+    assert all(torch._C._is_cow_tensor(o) for o in outs)
+    refused(STATE, c.append, 0, k, k, i(3), i(3), rope=rope, q=q, q_out=outs[0], k_out=outs[1])
+    refused(STATE, c.attend, 0, q, i(3, 2), i(3), outs[2], lse=outs[3])
+    assert not any(torch._C._is_cow_tensor(o) for o in outs)
+    inputs = [lazy(k), lazy(k), lazy(q)]                           # what is only read stays shared
+    refused(STATE, c.append, 0, inputs[0], inputs[1], i(3), i(3), rope=rope, q=inputs[2], q_out=q)
+    assert all(torch._C._is_cow_tensor(x) for x in inputs)
