@@ -568,6 +568,20 @@ def _closed(*args):
     raise KvpError(4, "the cache is closed")
 
 
+# Workspaces of caches that were closed without a wait for the device, by their ids: calls on other streams may still use them, and
+# PyTorch's allocator knows only of the stream that they were made on.
+_unwaited = {}
+
+
+def _wait_for(device: int):
+    """Waits for all work on the device.  Workspaces that had no wait until then may go."""
+    import torch
+    before = [i for i, w in list(_unwaited.items()) if w[0] == device]
+    torch.cuda.synchronize(device)
+    for i in before:
+        _unwaited.pop(i, None)
+
+
 class PagedCache:
     """``kvp_cache`` over the caller's page tensors: ``k``, ``v`` = [layer][page][kv head][row][d] (order "heads") or
     [layer][page][row][kv head][d] ("tokens"), with any strides.  CPU tensors make a host-only cache: pages are counted,
@@ -609,13 +623,14 @@ class PagedCache:
     def close(self):
         if self._h:
             self._append = self._attend = self._compact = _closed
+            h, self._h = self._h, ctypes.c_void_p()
+            self._L.kvp_cache_destroy(h)
             if self.workspace is not None:
                 # calls on other streams may still use it; while something is recorded nothing may be waited for
                 import torch
+                _unwaited[id(self.workspace)] = self.device, self.workspace
                 if not torch.cuda.is_current_stream_capturing():
-                    torch.cuda.synchronize(self.device)
-            self._L.kvp_cache_destroy(self._h)
-            self._h = ctypes.c_void_p()
+                    _wait_for(self.device)
 
     def __del__(self):
         try:

@@ -69,3 +69,30 @@ def test_compaction_of_tables_without_columns():
     c.compact(i(2, 0), ints([30, 0]), i(2, 0), kept, ints([20, 3]))
     torch.cuda.synchronize()
     assert torch.equal(k, was[0]) and torch.equal(v, was[1])
+
+
+def test_a_workspace_is_not_handed_out_while_calls_use_it():
+    """A cache with a call under way on another stream goes while a graph is recorded: its workspace is not handed out again until
+    a later close has waited for the device."""
+    k, v = ref.pages((1, 300, 2, 16, 128), "heads", torch.bfloat16, seed=3)
+    c, other = kvp.PagedCache(k, v, 8), kvp.PagedCache(k, v, 8)
+    q = torch.randn(1, 8, 128, device="cuda").bfloat16()
+    out, want, n = torch.empty_like(q), torch.empty_like(q), ints([4800])
+    table = torch.arange(300, dtype=torch.int32, device="cuda")[None]
+    other.attend(0, q, table, n, want)
+    torch.cuda.synchronize()
+    side, g, size = torch.cuda.Stream(), torch.cuda.CUDAGraph(), c.workspace.numel()
+    at = c.workspace.data_ptr()
+    x = torch.zeros(1, device="cuda")
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+    c.attend(0, q, table, n, out, stream=side)
+    with torch.cuda.graph(g):
+        x += 1
+        c.close()
+        del c
+    blocks = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    assert all(b.data_ptr() != at for b in blocks)
+    other.close()
+    assert side.query() and torch.equal(out, want)
+    assert not any(w.data_ptr() == at for _, w in kvp._unwaited.values())

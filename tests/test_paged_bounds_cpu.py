@@ -1,7 +1,9 @@
 """The paged cache's calls at the ends of their ranges, and what surrounds them, without a GPU."""
 import ctypes
+import gc
 import os
 import subprocess
+import weakref
 
 import pytest
 import torch
@@ -51,3 +53,62 @@ def test_outputs_are_separated_from_what_they_were_cloned_from():
     inputs = [lazy(k), lazy(k), lazy(q)]                           # what is only read stays shared
     refused(STATE, c.append, 0, inputs[0], inputs[1], i(3), i(3), rope=rope, q=inputs[2], q_out=q)
     assert all(torch._C._is_cow_tensor(x) for x in inputs)
+
+
+class _Recording:
+    """Stands in for the device of a host-only cache: whether something is recorded, and who waited for it."""
+
+    def __init__(self, monkeypatch):
+        self.recording, self.fails, self.waits = False, False, 0
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: self.recording)
+        monkeypatch.setattr(torch.cuda, "synchronize", self.wait)
+
+    def wait(self, device):
+        assert device == self.device and not self.recording
+        if self.fails:
+            raise RuntimeError("another thread records")
+        self.waits += 1
+
+    device = 99
+
+    def cache(self):
+        c = cache()
+        c.device, c.workspace = self.device, torch.zeros(8)
+        c.workspace.gone = weakref.ref(c.workspace)
+        return c, c.workspace.gone
+
+
+def test_a_workspace_outlives_calls_that_nobody_waited_for(monkeypatch):
+    """A cache that is closed, or dropped, while something is recorded cannot wait for its attend calls on other streams: its
+    workspace stays until somebody has waited for the device."""
+    dev = _Recording(monkeypatch)
+    closed, a = dev.cache()
+    dropped, b = dev.cache()
+    late, _ = dev.cache()
+    dev.recording = True
+    closed.close()
+    del closed, dropped
+    gc.collect()
+    assert a() is not None and b() is not None and dev.waits == 0
+    dev.recording = False
+    late.close()
+    gc.collect()
+    assert dev.waits == 1 and a() is None and b() is None
+
+
+def test_a_wait_that_fails_ends_the_cache_but_not_its_workspace(monkeypatch):
+    dev = _Recording(monkeypatch)
+    c, a = dev.cache()
+    dev.fails = True
+    with pytest.raises(RuntimeError):
+        c.close()
+    assert not c._h
+    c.close()                                              # there is nothing more to close
+    del c
+    gc.collect()
+    assert a() is not None
+    dev.fails = False
+    other, _ = dev.cache()
+    other.close()
+    gc.collect()
+    assert a() is None
