@@ -159,14 +159,14 @@ _calls = None
 
 
 def calls():
-    """The module that marshals the paged cache's calls on tensors (needs PyTorch); built like the library."""
+    """The module that marshals the paged cache's calls on tensors (needs PyTorch, of the version that it was built for); built
+    like the library."""
     global _calls
     if _calls is None:
-        import torch  # noqa: F401  (the module's symbols are in its libraries)
-        L = lib()
-        if not os.path.exists(_build.CALLS_PATH):
-            _build.build()
-        spec = importlib.util.spec_from_file_location("_kvp_calls", _build.CALLS_PATH)
+        L, path = lib(), _build.calls_path()
+        if not os.path.exists(path) or os.environ.get("KVP_REBUILD"):
+            path = _build.build_calls()
+        spec = importlib.util.spec_from_file_location("_kvp_calls", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.kvp_cache_append, L.kvp_cache_attend, L.kvp_cache_compact, L.kvp_norm_rope)))

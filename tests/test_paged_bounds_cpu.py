@@ -3,6 +3,8 @@ import ctypes
 import gc
 import os
 import subprocess
+import sys
+import sysconfig
 import weakref
 
 import pytest
@@ -112,3 +114,45 @@ def test_a_wait_that_fails_ends_the_cache_but_not_its_workspace(monkeypatch):
     other.close()
     gc.collect()
     assert a() is None
+
+
+# ---- what is built ------------------------------------------------------------------------------------------------------
+
+@pytest.fixture
+def compilers(monkeypatch, tmp_path):
+    """Compilers that note how they were called and leave an empty file."""
+    seen = []
+
+    def run(cmd, **kw):
+        seen.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+
+    monkeypatch.setattr(build.subprocess, "check_call", run)
+    monkeypatch.setattr(build, "_HERE", str(tmp_path))
+    monkeypatch.setattr(build, "CSRC", str(tmp_path / "csrc"))
+    monkeypatch.setattr(build, "LIB_PATH", str(tmp_path / "libkvp.so"))
+    (tmp_path / "csrc").mkdir()
+    (tmp_path.parent / "include").mkdir(exist_ok=True)
+    for f in (tmp_path / "csrc" / "kvp_calls.cpp", tmp_path.parent / "include" / "kvp.h"):
+        f.write_text("")
+        os.utime(f, (1, 1))
+    return seen
+
+
+def test_the_library_builds_without_pytorch(compilers, monkeypatch):
+    monkeypatch.setattr(build.importlib.util, "find_spec", lambda name: None)
+    monkeypatch.setitem(sys.modules, "torch", None)
+    assert build.build(force=True) == build.LIB_PATH and os.path.exists(build.LIB_PATH)
+    assert not any("kvp_calls" in str(x) for cmd in compilers for x in cmd)
+
+
+def test_another_pytorch_gets_a_module_of_its_own(compilers, monkeypatch):
+    first = build.build_calls()
+    assert os.path.exists(first) and len(compilers) == 1 and build.build_calls() == first and len(compilers) == 1
+    monkeypatch.setattr(torch, "__version__", "9.9.9+test")
+    second = build.build_calls()
+    assert second != first and os.path.exists(second) and len(compilers) == 2
+    assert sysconfig.get_config_var("EXT_SUFFIX") in first          # and another Python
+    os.utime(os.path.join(build.CSRC, "kvp_calls.cpp"))
+    os.utime(second, (2, 2))
+    assert build.build_calls() == second and len(compilers) == 3    # newer sources
