@@ -1,6 +1,6 @@
 """ctypes binding of ``libkvp.so`` - argument marshalling only; every step of the path runs in the
 library's CUDA kernels.  Function names mirror ``include/kvp.h``.  The paged cache's calls on tensors are marshalled by a
-module in C++ (``csrc/kvp_calls.cpp``); what it does not take is looked at here, and refused with the reason.
+module in C++ (``csrc/kvp_calls.cpp``); what it does not take is looked at here, and refused with the reason; where the module is not there, all calls are.
 
 PyTorch is used here for device memory and streams only (``Context`` accepts torch tensors and
 passes their ``data_ptr()``).  There is no CPU fallback: if the shared library is missing or cannot
@@ -12,6 +12,8 @@ import ctypes
 import importlib.util
 import os
 import struct
+import subprocess
+import warnings
 from typing import List, Optional, Sequence, Tuple
 
 from . import build as _build
@@ -158,18 +160,34 @@ EXPORTED = ["kvp_version", "kvp_token_bytes", "kvp_workspace_bytes", "kvp_create
 _calls = None
 
 
+class _NoModule:
+    """Takes no call, so that Python marshals all of them."""
+
+    @staticmethod
+    def append(*args):
+        return -1
+
+    attend = compact = norm_rope = append
+
+
 def calls():
     """The module that marshals the paged cache's calls on tensors (needs PyTorch, of the version that it was built for); built
-    like the library."""
+    like the library.  Where it can be neither built nor loaded, Python marshals them: 4 us more for each call, the same kernels."""
     global _calls
     if _calls is None:
-        L, path = lib(), _build.calls_path()
-        if not os.path.exists(path) or os.environ.get("KVP_REBUILD"):
-            path = _build.build_calls()
-        spec = importlib.util.spec_from_file_location("_kvp_calls", path)
-        module = importlib.util.module_from_spec(spec)
-        spec.loader.exec_module(module)
-        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.kvp_cache_append, L.kvp_cache_attend, L.kvp_cache_compact, L.kvp_norm_rope)))
+        L = lib()
+        try:
+            path = _build.calls_path()
+            if not os.path.exists(path) or os.environ.get("KVP_REBUILD"):
+                path = _build.build_calls()
+            spec = importlib.util.spec_from_file_location("_kvp_calls", path)
+            module = importlib.util.module_from_spec(spec)
+            spec.loader.exec_module(module)
+        except (ImportError, OSError, subprocess.SubprocessError) as e:
+            warnings.warn(f"the paged cache's calls are marshalled in Python: {e}", RuntimeWarning)
+            module = _NoModule
+        else:
+            module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.kvp_cache_append, L.kvp_cache_attend, L.kvp_cache_compact, L.kvp_norm_rope)))
         _calls = module
     return _calls
 

@@ -96,3 +96,29 @@ def test_a_workspace_is_not_handed_out_while_calls_use_it():
     other.close()
     assert side.query() and torch.equal(out, want)
     assert not any(w.data_ptr() == at for _, w in kvp._unwaited.values())
+
+
+def test_python_marshals_the_same_calls(monkeypatch):
+    """The bits of every call do not depend on who marshals it."""
+    def run():
+        k, v = ref.pages((2, 40, 2, 16, 64), "heads", torch.bfloat16, seed=4)
+        c = kvp.PagedCache(k, v, 8, max_batch=2)
+        g = torch.Generator(device="cuda").manual_seed(4)
+        x = torch.randn(5, 12, 64, generator=g, device="cuda").bfloat16()
+        q, kn, vn = x[:, :8], x[:, 8:10], x[:, 10:]
+        w, rope, pos = (1 + torch.rand(64, generator=g, device="cuda")).bfloat16(), kvp.Rope(64, rotary_dim=48, theta=1e6), ints([9, 1 << 30, 0, 7, 300])
+        q1, k1, q2, out = (torch.empty(5, h, 64, device="cuda", dtype=torch.bfloat16) for h in (8, 2, 8, 8))
+        lse, table = torch.empty(2, 8, device="cuda"), torch.arange(16, dtype=torch.int32, device="cuda").view(2, 8)
+        c.append(1, kn, vn, pos, ints([3, 40, 41, 42, 99]), rope=rope, q=q, q_out=q1, k_out=k1, q_weight=w, k_weight=w)
+        c.append(0, kn, vn, None, ints([3, 40, 41, 42, 99]))
+        kvp.norm_rope(q, None, pos, rope, q2, q_weight=w)
+        c.attend(1, q1[:2], table, ints([128, 77]), out[:2], lse=lse, first=ints([0, 40]))
+        c.attend(0, q1[2:4], table, ints([128, 77]), out[2:4])
+        c.compact(table, ints([128, 77]), table + 16, torch.arange(1, 31, dtype=torch.int32, device="cuda").expand(2, 1, 2, 30).contiguous(), ints([30, 4]))
+        return k, v, q1, k1, q2, out[:4], lse
+
+    want = run()
+    assert hasattr(kvp.calls(), "bind")
+    monkeypatch.setattr(kvp, "_calls", kvp._NoModule)
+    for a, b in zip(run(), want):
+        assert torch.equal(a, b)

@@ -12,7 +12,8 @@ import torch
 
 from paper_2604_13226_b200 import binding as kvp
 from paper_2604_13226_b200 import build
-from test_paged_cpu import CAPACITY, INVALID, STATE, cache, refused
+import test_paged_cpu
+from test_paged_cpu import INVALID, STATE, cache, refused
 
 
 def test_tiles_of_the_longest_lists(tmp_path):
@@ -156,3 +157,31 @@ def test_another_pytorch_gets_a_module_of_its_own(compilers, monkeypatch):
     os.utime(os.path.join(build.CSRC, "kvp_calls.cpp"))
     os.utime(second, (2, 2))
     assert build.build_calls() == second and len(compilers) == 3    # newer sources
+
+
+def _no_compiler(force=False):
+    raise subprocess.CalledProcessError(1, ["g++"])
+
+
+def _cut_short(force=False):
+    path = build.calls_path()
+    open(path, "wb").write(b"\x7fELF")
+    return path
+
+
+@pytest.mark.parametrize("why", [_no_compiler, _cut_short])
+def test_python_marshals_where_the_module_is_not(monkeypatch, tmp_path, why):
+    """What the module refuses, and what it hands on, does not depend on its being there."""
+    monkeypatch.setattr(kvp, "_calls", None)
+    monkeypatch.setattr(build, "calls_path", lambda: str(tmp_path / "none.so"))
+    monkeypatch.setattr(build, "build_calls", why)
+    with pytest.warns(RuntimeWarning, match="marshalled in Python"):
+        cache().close()
+    assert kvp.calls() is kvp._NoModule
+    for test in (test_paged_cpu.test_append_arguments, test_paged_cpu.test_attend_arguments, test_paged_cpu.test_compact_arguments,
+                 test_paged_cpu.test_rope_arguments, test_compaction_of_tables_without_columns):
+        test()
+    c = cache()
+    c.close()
+    i = torch.zeros(3, dtype=torch.int32)
+    refused(STATE, c.append, 0, torch.zeros(3, 2, 64), torch.zeros(3, 2, 64), i, i)
