@@ -204,6 +204,20 @@ def _i32_packed(xs: List[int]):
         return _i32_array(xs)
 
 
+def _i32(x: int, name: str) -> int:
+    """``x``, which ctypes would cut to 32 bits without a word."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise KvpError(1, f"{name}: {x} is not a number of 32 bits")
+    return x
+
+
+def _i32_list(xs: Sequence[int], name: str):
+    try:
+        return struct.pack(f"{len(xs)}i", *xs)
+    except struct.error:
+        return _i32_array([_i32(x, name) for x in xs])
+
+
 def _ptr(t) -> Optional[int]:
     """Device (or host) address of a torch tensor / int / None."""
     if t is None:
@@ -464,7 +478,7 @@ class Rope:
                  low_rotations: float = 1.0, high_rotations: float = 4.0, magnitude: float = 1.0):
         r = kvp_rope()
         r.struct_bytes = ctypes.sizeof(kvp_rope)
-        r.pairing, r.rotary_dim = pairing, head_dim if rotary_dim is None else rotary_dim
+        r.pairing, r.rotary_dim = _i32(pairing, "pairing"), _i32(head_dim if rotary_dim is None else rotary_dim, "rotary_dim")
         r.theta, r.scale, r.original_positions = theta, scale, original_positions
         r.low_rotations, r.high_rotations, r.magnitude = low_rotations, high_rotations, magnitude
         self._inv_freq = None
@@ -523,7 +537,7 @@ def _table(t, device: int, n: int, name: str):
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or shape[0] != n or t.dtype is not _int32() or t.get_device() != device or (stride[1] != 1 and shape[1] > 1):
         raise KvpError(1, f"{name}: {tuple(shape)} with strides {stride}, {t.dtype} on {t.device}, not [{n}][pages] of int32")
-    return t.data_ptr(), stride[0], shape[1]
+    return t.data_ptr(), stride[0], _i32(shape[1], name)
 
 
 _int32_dtype = None
@@ -546,7 +560,7 @@ def _tokens(dtype, device: int, d: int, q, k, v, q_out, k_out, positions, slots,
     first = q if q is not None else k
     if first is None:
         raise KvpError(1, "neither q nor k")
-    n = first.shape[0]
+    n = _i32(first.shape[0], "tokens")
     none = (0, 0, 0, 0)
     qp, hq, q0, q1 = none if q is None else _rows(q, dtype, device, d, n, "q")
     kp, hk, k0, k1 = none if k is None else _rows(k, dtype, device, d, n, "k")
@@ -621,6 +635,8 @@ class PagedCache:
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or _raw_stream
         self.device = k.device.index if k.device.type == "cuda" else -1
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape[0], k.shape[1], k.shape[head], k.shape[row], k.shape[4]
+        for n, name in ((n_q_heads, "n_q_heads"), (max_batch, "max_batch"), *((n, "size") for n in k.shape)):
+            _i32(n, name)
         self.n_q_heads, self.max_batch = n_q_heads, max_batch
         c = kvp_cache_config()
         c.struct_bytes, c.device, c.n_layers, c.n_q_heads, c.n_kv_heads = ctypes.sizeof(c), self.device, self.n_layers, n_q_heads, self.n_kv_heads
@@ -677,6 +693,7 @@ class PagedCache:
         if rc > 0:
             self._check(rc)
         # the tensors do not fit one another or the cache: what is wrong is found, and said, here
+        _i32(layer, "layer")
         if k is None or v is None or slots is None:
             raise KvpError(1, "append: k, v and slots are needed")
         a = _tokens(self.dtype, self.device, self.head_dim, q, k, v, q_out, k_out, positions, slots, q_weight, k_weight, eps)
@@ -691,7 +708,8 @@ class PagedCache:
             return
         if rc > 0:
             self._check(rc)
-        n, dev, dtype, d = q.shape[0], self.device, self.dtype, self.head_dim
+        _i32(layer, "layer")
+        n, dev, dtype, d = _i32(q.shape[0], "requests"), self.device, self.dtype, self.head_dim
         qp, hq, q0, q1 = _rows(q, dtype, dev, d, n, "q")
         op, ho, o0, o1 = _rows(out, dtype, dev, d, n, "out")
         if hq != self.n_q_heads or ho != hq:
@@ -707,8 +725,8 @@ class PagedCache:
         """The first rows[i] rows (None: all) of page src[i] to page dst[i], in all layers."""
         if len(src) != len(dst) or (rows is not None and len(rows) != len(src)):
             raise KvpError(1, "copy: lists of different lengths")
-        self._check(self._L.kvp_cache_copy(self._h, len(src), _i32_packed(src), _i32_packed(dst),
-                                           None if rows is None else _i32_packed(rows), self._stream(stream)))
+        self._check(self._L.kvp_cache_copy(self._h, len(src), _i32_list(src, "page"), _i32_list(dst, "page"),
+                                           None if rows is None else _i32_list(rows, "rows"), self._stream(stream)))
 
     def compact(self, table, lens, new_table, kept, n_kept, stream=None):
         """Row i < n_kept[b] of new_table[b]'s pages becomes row kept[b][l][h][i] of table[b]'s; kept = [request][layer or
@@ -718,7 +736,7 @@ class PagedCache:
             return
         if rc > 0:
             self._check(rc)
-        n, dev = n_kept.shape[0], self.device
+        n, dev = _i32(n_kept.shape[0], "requests"), self.device
         shape, stride = kept.shape, kept.stride()
         if len(shape) != 4 or shape[0] != n or kept.dtype is not _int32() or kept.get_device() != dev or (stride[3] != 1 and shape[3] > 1):
             raise KvpError(1, f"kept: {tuple(shape)} with strides {stride}, {kept.dtype} on {kept.device}")
@@ -728,28 +746,28 @@ class PagedCache:
         tp, t0, cols = _table(table, dev, n, "table")
         np, n0, new_cols = _table(new_table, dev, n, "new_table")
         self._check(self._L.kvp_cache_compact(self._h, n, tp, t0, cols, _ints(lens, dev, (n,), "lens"), np, n0, new_cols, kept.data_ptr(),
-                                              strides, shape[3], _ints(n_kept, dev, (n,), "n_kept"), self._stream(stream)))
+                                              strides, _i32(shape[3], "kept"), _ints(n_kept, dev, (n,), "n_kept"), self._stream(stream)))
 
     # -- pages -----------------------------------------------------------------------------------
     def take(self, n: int) -> List[int]:
-        out = (ctypes.c_int32 * max(1, n))()
+        out = (ctypes.c_int32 * max(1, min(_i32(n, "pages"), self.n_pages)))()     # (no more can be taken)
         self._check(self._L.kvp_cache_take(self._h, n, out))
         return list(out)[:n]
 
     def share(self, pages: Sequence[int]):
-        self._check(self._L.kvp_cache_share(self._h, len(pages), _i32_packed(pages)))
+        self._check(self._L.kvp_cache_share(self._h, len(pages), _i32_list(pages, "page")))
 
     def release(self, pages: Sequence[int]):
-        self._check(self._L.kvp_cache_release(self._h, len(pages), _i32_packed(pages)))
+        self._check(self._L.kvp_cache_release(self._h, len(pages), _i32_list(pages, "page")))
 
     def fork(self, pages: Sequence[int], n_tokens: int, n_forks: int = 1, stream=None) -> List[List[int]]:
         """``n_forks`` page lists for the first ``n_tokens`` rows of ``pages``: whole pages are shared, a last one that is not
         full is copied to a new page for each."""
-        cols = -(-n_tokens // self.page_size)
+        cols = -(-_i32(n_tokens, "tokens") // self.page_size)
         if cols > len(pages):
             raise KvpError(1, f"fork: {n_tokens} tokens in {len(pages)} pages of {self.page_size}")
-        out = (ctypes.c_int32 * max(1, n_forks * cols))()
-        self._check(self._L.kvp_cache_fork(self._h, n_tokens, _i32_packed(pages), n_forks, out, self._stream(stream)))
+        out = (ctypes.c_int32 * max(1, _i32(n_forks, "forks") * cols))()
+        self._check(self._L.kvp_cache_fork(self._h, n_tokens, _i32_list(pages, "page"), n_forks, out, self._stream(stream)))
         return [list(out[f * cols:(f + 1) * cols]) for f in range(n_forks)]
 
     @property

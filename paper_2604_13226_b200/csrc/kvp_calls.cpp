@@ -76,10 +76,13 @@ bool vector_of(PyObject *o, const wanted &w, const void *&p)
     return true;
 }
 
-bool cache_of(PyObject *const *args, void *&handle, int32_t &layer, wanted &w)
+// False: an exception is set
+bool cache_of(PyObject *const *args, void *&handle, int32_t &layer, bool &fits, wanted &w)
 {
     handle = PyLong_AsVoidPtr(args[0]);
-    layer = (int32_t)PyLong_AsLong(args[1]);
+    const long number = PyLong_AsLong(args[1]);
+    fits = number == (int32_t)number;
+    layer = (int32_t)number;
     w.type = PyLong_AsLong(args[2]) == KVP_DTYPE_BF16 ? c10::kBFloat16 : c10::kFloat;
     w.device = (int)PyLong_AsLong(args[3]);
     w.d = PyLong_AsLong(args[4]);
@@ -95,7 +98,8 @@ PyObject *append(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     void *handle;
     int32_t layer;
     wanted w;
-    if (!cache_of(args, handle, layer, w)) return nullptr;
+    bool fits;
+    if (!cache_of(args, handle, layer, fits, w)) return nullptr;
     kvp_tokens t = {};
     t.struct_bytes = sizeof t;
     const void *rope = given(args[9]) ? PyLong_AsVoidPtr(args[9]) : nullptr;
@@ -103,9 +107,8 @@ PyObject *append(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     void *stream = given(args[16]) ? PyLong_AsVoidPtr(args[16]) : nullptr;
     if (PyErr_Occurred()) return nullptr;
     int64_t n = -1, hq = -1, hkv = -1;
-    bool fits = true;
     try {
-        fits = (!given(args[11]) || rows(args[11], w, n, hq, t.q_out, t.q_out_stride)) && (!given(args[12]) || rows(args[12], w, n, hkv, t.k_out, t.k_out_stride)) &&
+        fits = fits && (!given(args[11]) || rows(args[11], w, n, hq, t.q_out, t.q_out_stride)) && (!given(args[12]) || rows(args[12], w, n, hkv, t.k_out, t.k_out_stride)) &&
                rows(args[5], w, n, hkv, t.k, t.k_stride) && rows(args[6], w, n, hkv, t.v, t.v_stride) && n <= INT32_MAX && hkv <= INT32_MAX &&
                (!given(args[7]) || ints(args[7], w.device, n, t.positions)) && ints(args[8], w.device, n, t.slots) &&
                (!given(args[10]) || rows(args[10], w, n, hq, t.q, t.q_stride)) && hq <= INT32_MAX &&
@@ -127,7 +130,8 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     void *handle;
     int32_t layer;
     wanted w;
-    if (!cache_of(args, handle, layer, w)) return nullptr;
+    bool fits;
+    if (!cache_of(args, handle, layer, fits, w)) return nullptr;
     int64_t hq = PyLong_AsLong(args[5]), n = -1, cols = 0, table_stride = 0, q_stride[2], out_stride[2];
     void *stream = given(args[12]) ? PyLong_AsVoidPtr(args[12]) : nullptr;
     if (PyErr_Occurred()) return nullptr;
@@ -135,9 +139,8 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     void *out = nullptr;
     const int32_t *table = nullptr, *lens = nullptr, *first = nullptr;
     float *lse = nullptr;
-    bool fits = true;
     try {
-        fits = rows(args[7], w, n, hq, out, out_stride) && rows(args[6], w, n, hq, q, q_stride) && n <= INT32_MAX &&
+        fits = fits && rows(args[7], w, n, hq, out, out_stride) && rows(args[6], w, n, hq, q, q_stride) && n <= INT32_MAX &&
                ints(args[8], w.device, n, table, &cols, &table_stride) && cols <= INT32_MAX && ints(args[9], w.device, n, lens) &&
                (!given(args[10]) || ints(args[10], w.device, n, first));
         if (fits && given(args[11])) {

@@ -117,6 +117,35 @@ def test_a_wait_that_fails_ends_the_cache_but_not_its_workspace(monkeypatch):
     assert a() is None
 
 
+@pytest.mark.parametrize("module", [True, False])
+def test_numbers_beyond_32_bits_are_not_cut_to_them(monkeypatch, module):
+    """2^32 + 1 is not 1: layers, pages, rows, counts and sizes."""
+    if not module:
+        monkeypatch.setattr(kvp, "_calls", kvp._NoModule)
+    far = (2 ** 32, 2 ** 32 + 1, -2 ** 32, 2 ** 31)
+    c = cache(layers=2, heads=2, hq=4, pages=8, size=4)
+    t, i = (lambda *s: torch.zeros(s)), (lambda *s: torch.zeros(s, dtype=torch.int32))
+    k, q, p = t(3, 2, 64), t(3, 4, 64), c.take(2)
+    for x in far:
+        refused(INVALID, c.append, x, k, k, None, i(3))
+        refused(INVALID, c.attend, x, q, i(3, 2), i(3), q)
+        refused(INVALID, c.copy, [x], [3])
+        refused(INVALID, c.copy, [3], [x])
+        refused(INVALID, c.copy, [3], [4], [x])
+        refused(INVALID, c.share, [x + p[0]])
+        refused(INVALID, c.release, [x + p[0]])
+        refused(INVALID, c.fork, [x + p[0]], 4)
+        refused(INVALID, c.fork, p, 4, x)
+        refused(INVALID, c.take, x)
+        refused(INVALID, cache, hq=4 + x)
+        refused(INVALID, cache, max_batch=4 + x)
+        refused(INVALID, kvp.Rope, 64, rotary_dim=x + 64)
+        refused(INVALID, kvp.Rope, 64, pairing=x)
+    refused(INVALID, c.fork, p, 2 ** 32)
+    assert c.free_pages == 6
+    refused(STATE, c.append, 1, k, k, None, i(3))
+
+
 # ---- what is built ------------------------------------------------------------------------------------------------------
 
 @pytest.fixture
