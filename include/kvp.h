@@ -423,8 +423,11 @@ KVP_API int32_t kvp_compose_noalloc(const void *pool_k, const void *pool_v, int6
  *   original_positions = L: with t = L f_i / 2 pi the turns that pair i makes over the original context, pairs of at least
  *   high_rotations turns keep f_i, pairs of at most low_rotations get f_i / scale, and between them
  *   w f_i + (1 - w) f_i / scale with w = (t - low_rotations) / (high_rotations - low_rotations).  (1, 4) with magnitude 1 is
- *   the scaling of Llama 3.1, (1, 32) with magnitude 0.1 ln(scale) + 1 that of YaRN (Peng et al. 2023, Section 3).
- * Angles are formed in double precision, position * f_i / 2 pi reduced to a part of a turn there.
+ *   the scaling of Llama 3.1, (1, 32) with magnitude 0.1 ln(scale) + 1 that of YaRN as its paper states it (Peng et al. 2023,
+ *   Section 3).  Programs whose ramp runs over the pair's index i between two rounded bounds, instead of over its turns, give
+ *   other frequencies: models trained with those pass them as inv_freq, with scale 1.
+ * Angles are formed in double precision, position * f_i / 2 pi reduced to a part of a turn there and rounded to 2^-26 turns;
+ * beyond positions of about 2^28 the double product's own rounding is larger, 2^-24 turns at 2^31.
  */
 typedef struct kvp_rope {
     int32_t struct_bytes;       /* = sizeof(kvp_rope)                                                 */

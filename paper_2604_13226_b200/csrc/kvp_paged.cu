@@ -67,7 +67,9 @@ struct append_args {
 // a token, or a part of its heads: the token's angles are formed once, and the sines, cosines and weights that a thread needs
 // stay in its registers for all heads (read from shared memory for each head they took twice the wavefronts of the rows
 // themselves).  The angle is formed in double precision, as a part of a turn, and its sine and cosine from the rounded
-// remainder: |remainder| <= 1/2 turn, so the rounding moves the angle by 2^-25 turns at most, wherever the position lies.
+// remainder: |remainder| <= 1/2 turn, so that rounding moves the angle by 2^-26 turns at most, wherever the position lies (rows of
+// fp32 4.3e-8 off in the 2-norm, 3.9e-8 with sines and cosines rounded from 64 bits).  The product in front of it is exact to
+// 2^-53 of itself: less than that up to positions of 2^28, 2^-24 turns at 2^31.
 template <typename T, int D> struct row_math {
     static constexpr int EV = elem<T>::kPerVec, P = EV / 2, L = D / EV / 2, R = 32 / L;   // elements and pairs of a word, threads of a row, rows of a warp
     int w0, w1;                            // the words
@@ -319,7 +321,8 @@ kvp_divisor divisor(int32_t d)
 template <typename T, int D>
 cudaError_t launch_append(append_args &a, int sm_count, cudaStream_t st)
 {
-    // 512 tokens of 32/8 heads: 7.1 us as many, 4.9 as few; 1,000 of 28/4: 6.1, 11.4.  Twice as many blocks as fit, so that the last
+    // 512 tokens of 32/8 heads: 7.1 us as many, 4.9 as few; 1,000 of 28/4: 6.1, 11.4 (fewer heads, whose tokens are less work,
+    // were not measured at these borders).  Twice as many blocks as fit, so that the last
     // ones even out (one wave: 8,000 tokens of fp32 73 us instead of 65).
     if (a.n_tokens >= 4 * sm_count) {
         if (a.n_tokens <= 8 * sm_count) {

@@ -64,7 +64,9 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
-// 16 bytes to shared memory; without `there` zeros, and src is not read
+// 16 bytes to shared memory; without `there` zeros, and src is not read.  L2 fetches 256 bytes at a time: that is two rows of bf16
+// heads of 64, the other one the next row's (pages by head: 146 requests of 674-8,335 rows, 32/8 heads, 239 us of a floor of 221)
+// or another head's, which is read much later (pages by token: 339 us).
 __device__ __forceinline__ void copy16(uint32_t dst, const char *src, bool there)
 {
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -845,7 +847,8 @@ cudaError_t launch_any(const kvp_paged_args &a, int sm_count, cudaStream_t st)
     // CTAs of 8 warps, one per SM, halve the parts that a unit is joined from: 8 x 8,000 rows of one kv head with 16 query heads
     // 27 -> 20 us, 133,120 rows 92.5 -> 90.0.  CTAs of 4 join within themselves more cheaply and hide one another's ends: 256 x
     // 200 rows 64 -> 48 us, 2,785 rows 9.7 -> 9.1, 16 x 16,000 rows of fp32 heads of 64 92 -> 86.  The lengths are not known
-    // here; tables for long lists mean long ones.
+    // here; tables for long lists mean long ones.  Where they do not, tables of 133,120 rows as a recorded step has them: 433 rows
+    // 7.2 -> 6.7 us, 2,785 8.8 -> 8.3, 8 x 2,000 17.9 -> 18.2, 16 x 2,000 27.6 -> 28.6, 16 x 433 11.1 -> 11.9.
     const bool eight = units < 2 * sm_count && (WIDE || (sizeof(T) == 2 && tiles >= 200ll * sm_count));
     return eight ? launch<T, D, WIDE, 8>(a, units, sm_count, st) : launch<T, D, WIDE, 4>(a, units, sm_count, st);
 }
